@@ -707,3 +707,13 @@ class IVFPQ:
 
     def norms(self):
         return vs_ivfpq_get_norms(self.h, self.device)
+
+    def attend(self, q, nprobe, scale, v0=0, limits=None):
+        """Attention over the stored vectors (4-bit codes, inner product): see vs_ivfpq_attend."""
+        from . import softmax
+        return softmax.vs_ivfpq_attend(self.h, self.d, q, nprobe, scale, v0, limits)
+
+    def attend_grad(self, q, nprobe, scale, lse, g_out, g_lse=None, v0=0, limits=None):
+        """The gradient of attend for q: see vs_ivfpq_attend_grad."""
+        from . import softmax
+        return softmax.vs_ivfpq_attend_grad(self.h, self.d, q, nprobe, scale, lse, g_out, g_lse, v0, limits)

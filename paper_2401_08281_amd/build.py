@@ -12,7 +12,13 @@ CALIBRATE_SOURCE = "calibrate.hip"
 SOURCES = ["api.hip", "kernels_dist.hip", "kernels_select.hip", "kernels_ivfpq.hip", "kernels_mfma.hip", "kernels_nearest.hip",
            "kernels_refine.hip", "kernels_train.hip",
            "kernels_ivfflat.hip", "kernels_mscan.hip", "kernels_place.hip"]
-HEADERS = ["common.hpp", "internal.hpp", "survivors.hpp", os.path.join("..", "..", "include", "vs.h")]
+# the softmax operators over the rows of an index (include/vs_softmax.h): a library beside libvs.so,
+# which it asks for the coarse quantizer
+SOFTMAX_LIB = os.path.join(HERE, "libvs_softmax.so")
+SOFTMAX_SOURCES = ["softmax_api.hip", "kernels_logprob.hip", "kernels_attend.hip"]
+SOFTMAX_HEADERS = ["common.hpp", "internal.hpp", "store.hpp", "softmax.hpp",
+                   os.path.join("..", "..", "include", "vs.h"), os.path.join("..", "..", "include", "vs_softmax.h")]
+HEADERS = ["common.hpp", "internal.hpp", "store.hpp", "survivors.hpp", os.path.join("..", "..", "include", "vs.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fvisibility=hidden",
@@ -30,12 +36,24 @@ def calibrate_lib_path():
     return CALIBRATE_LIB
 
 
-def is_stale():
-    if not os.path.exists(LIB):
+def softmax_lib_path():
+    return SOFTMAX_LIB
+
+
+def _older(lib, sources):
+    if not os.path.exists(lib):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    t = os.path.getmtime(lib)
+    deps = [os.path.join(CSRC, s) for s in sources] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
+
+
+def is_stale():
+    return _older(LIB, SOURCES + HEADERS)
+
+
+def softmax_is_stale():
+    return _older(SOFTMAX_LIB, SOFTMAX_SOURCES + SOFTMAX_HEADERS)
 
 
 def build_calibrate_lib(verbose=False):
@@ -46,6 +64,26 @@ def build_calibrate_lib(verbose=False):
         print(" ".join(cmd), flush=True)
     _drain([(cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT))])
     return CALIBRATE_LIB
+
+
+def build_softmax_lib(verbose=False):
+    """Compiles and links libvs_softmax.so, which finds libvs.so in its own folder."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    objs, procs = [], []
+    for src in SOFTMAX_SOURCES:
+        obj = os.path.join(CSRC, src.replace(".hip", ".o"))
+        cmd = [hipcc] + FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+        objs.append(obj)
+    _drain(procs)
+    cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", SOFTMAX_LIB] + objs + \
+        ["-L" + HERE, "-l:libvs.so", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return SOFTMAX_LIB
 
 
 def build_lib(verbose=False, jobs=4, extra_flags=(), out=None, tag=""):
@@ -70,6 +108,7 @@ def build_lib(verbose=False, jobs=4, extra_flags=(), out=None, tag=""):
     subprocess.run(cmd, check=True)
     if out is None and not tag:
         build_calibrate_lib(verbose)
+        build_softmax_lib(verbose)
     return target
 
 

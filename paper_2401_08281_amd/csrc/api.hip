@@ -12,6 +12,7 @@
 
 #include "../../include/vs.h"
 #include "internal.hpp"
+#include "store.hpp"
 
 namespace {
 
@@ -350,21 +351,12 @@ int knn_run(const KnnPlan& plan, char* ws, const float* A, int64_t na, const flo
 
 }  // namespace
 
-struct vs_ivfpq {
-  IvfpqDims g{};
-  int device = 0;
-  float* centroids = nullptr;   // [nlist, d]
-  float* codebooks = nullptr;   // [M, K, dsub]
-  int64_t ntotal = 0;
-  uint8_t* codes = nullptr;     // [ntotal, code_size], list-contiguous
-  int64_t* ids = nullptr;       // [ntotal], behind codes
+struct vs_ivfpq : IvfStore {
   float* norms = nullptr;       // [ntotal] squared norms of the decoded vectors, search_type 1 only
   float* cnorm = nullptr;       // [nlist] squared norms of the centroids (IVF-PQ only)
   float* list_tables = nullptr; // [nlist, K, M] per-list terms of the split tables (search type 2, once computed)
   int search_type = VS_ST_RESIDUAL_TABLES;
-  int64_t* list_off = nullptr;  // device [nlist + 1]
   std::vector<int64_t> h_off;   // host copy
-  int64_t max_list = 0;         // the longest list's length
   double crowding = 0.0;        // length of a stored vector's list, on average, over the mean length of a list
   float ms_slack = 0.f;         // one-hot rows: error bound of a sum over its spread, nine of ten sampled tables at most
   void* ms_mem = nullptr;       // what the matrix-core scan of the lists keeps (shapes that have one), behind centroids

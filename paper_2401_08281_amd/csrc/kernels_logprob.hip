@@ -1,0 +1,1057 @@
+// Softmax over the rows of a matrix: scores on the matrix cores with the softmax statistics in the
+// epilogue (the nq x nb scores are never stored), and the gradients, which compute them again.
+//
+// Orientation.  A tile is 128 rows of x (operand A) by 128 queries (operand B): in the accumulators of
+// v_mfma_f32_32x32x16 a lane then holds ONE query (column = lane & 31) and 16 rows per block
+// (row = (r & 3) + 8 (r >> 2) + 4 (lane >> 5)), so maxima and sums over rows are register arithmetic with a single
+// exchange between lane and lane ^ 32.
+#include "../../include/vs_softmax.h"
+#include "common.hpp"
+#include "softmax.hpp"
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+// e^t for t <= 0 (v_exp_f32: one unit in the last place, results below 2^-126 flush to 0 or a denormal, both fine here)
+__device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
+
+// One score t below the maximum of its group: its weight into l, weight times t into h.  Scores of -inf weigh nothing; a
+// NaN stays one in l.
+__device__ __forceinline__ void softmax_add(float t, float* l, float* h) {
+  const float e = exp_neg(t);
+  *l += e;
+  *h = __builtin_fmaf(e, fmaxf(t, -1000.f), *h);
+}
+// Group (m, l, h) under the maximum `top` of several groups.  A group without rows has l = 0 (or NaN).
+__device__ __forceinline__ void softmax_join(float top, float m, float gl, float gh, float* l, float* h) {
+  if (m == -__builtin_inff()) { *l += gl; return; }
+  const float t = m - top, e = exp_neg(t);
+  *l = __builtin_fmaf(gl, e, *l);
+  if (e > 0.f) *h = __builtin_fmaf(e, __builtin_fmaf(gl, t, gh), *h);
+}
+
+template <int DT> struct Elem;
+template <> struct Elem<0> { typedef float T; };
+template <> struct Elem<1> { typedef _Float16 T; };
+template <> struct Elem<2> { typedef __bf16 T; };
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v) { return (float)v; }
+
+// The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
+// not wait for them, and the compiler, which counts the wait states in between, has left them out where it copied an
+// accumulator at the start of the block behind the loop (v_accvgpr_read one instruction after the product: a stale
+// value).  20 wait states cover the 16 passes of a 32x32x16 product.
+__device__ __forceinline__ void settle_products() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// ---- tiles -------------------------------------------------------------------------
+// One K block (128 bytes) of 128 rows of each operand is a stage of 2 x 16 KB; two stages alternate, the next is
+// requested straight into LDS (global_load_lds_dwordx4) before the products of the present one.  A row's eight 16-byte
+// pieces are stored at piece ^ (row & 7): a fragment read (32 rows x 2 pieces) then touches every bank evenly.
+// With two planes a block holds 32 heads and their 32 tails, and one stage feeds hi*hi + hi*lo + lo*hi.
+constexpr int kStage = 2 * kSmTile * 128;
+constexpr int kTileLds = 2 * kStage;
+
+template <int PLANES, bool BF16>
+struct TileMul {
+  static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (BF16)
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  // acc[ib][jb] of this wavefront: rows 64 wa + 32 ib .., queries 64 wb + 32 jb ..
+  static __device__ __forceinline__ void run(const SmMatrix& A, int64_t a0, const SmMatrix& B, int64_t b0, int64_t kb0,
+                                             int64_t kb1, char* lds, f32x16 (&acc)[2][2]) {
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int wa = wave & 1, wb = wave >> 1;
+    // rows past the last one repeat it: their results are dropped
+    const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
+    const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
+    const int ra_max = (int)(A.rows - 1 - a0 < kSmTile ? A.rows - 1 - a0 : kSmTile - 1);
+    const int rb_max = (int)(B.rows - 1 - b0 < kSmTile ? B.rows - 1 - b0 : kSmTile - 1);
+    const char* ga[4];
+    const char* gb[4];
+    const int piece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = (wave * 4 + i) * 8 + (lane >> 3);
+      ga[i] = pa + (int64_t)(r < ra_max ? r : ra_max) * A.row_bytes + kb0 * 128 + piece * 16;
+      gb[i] = pb + (int64_t)(r < rb_max ? r : rb_max) * B.row_bytes + kb0 * 128 + piece * 16;
+    }
+    auto request = [&](int stage) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ga[i],
+                                         (__attribute__((address_space(3))) void*)(lds + stage * kStage + (wave * 4 + i) * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)gb[i],
+                                         (__attribute__((address_space(3))) void*)(lds + stage * kStage + kStage / 2 + (wave * 4 + i) * 1024), 16, 0, 0);
+        ga[i] += 128;
+        gb[i] += 128;
+      }
+    };
+    const int ra = (wa * 64 + (lane & 31)) * 128, rb = (wb * 64 + (lane & 31)) * 128, half = lane >> 5, sw = lane & 7;
+    request(0);
+    const int n = (int)(kb1 - kb0);
+    for (int t = 0; t < n; ++t) {
+      __syncthreads();                                  // the stage has landed, the other one is free
+      const char* s = lds + (t & 1) * kStage;
+      u32x4 a[2][4], b[2][4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const int off = ((2 * ks + half) ^ sw) * 16;
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib) {
+          a[ib][ks] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 128 + off);
+          b[ib][ks] = *reinterpret_cast<const u32x4*>(s + kStage / 2 + rb + ib * 32 * 128 + off);
+        }
+      }
+      if (t + 1 < n) request((t + 1) & 1);
+#pragma unroll
+      for (int ks = 0; ks < (PLANES == 2 ? 2 : 4); ++ks)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+          for (int jb = 0; jb < 2; ++jb) {
+            acc[ib][jb] = mul(a[ib][ks], b[jb][ks], acc[ib][jb]);
+            if constexpr (PLANES == 2) {
+              acc[ib][jb] = mul(a[ib][ks], b[jb][ks + 2], acc[ib][jb]);
+              acc[ib][jb] = mul(a[ib][ks + 2], b[jb][ks], acc[ib][jb]);
+            }
+          }
+    }
+    __syncthreads();                                    // LDS is free for the epilogue
+  }
+};
+
+// Workgroup number -> tile.  Workgroups go round the 8 XCDs; every XCD takes a contiguous run of tiles, column blocks of
+// 8 x 8 tiles inside it, so that the operands of the tiles in flight on one XCD meet in its L2.
+__device__ __forceinline__ void tile_of(int64_t wg, int64_t ta, int64_t tb, int64_t* a, int64_t* b) {
+  const int64_t n = ta * tb, per = (n + 7) / 8, big = n % 8 == 0 ? 8 : n % 8;   // XCDs with `per` tiles, others per - 1
+  const int64_t xcd = wg & 7, i = wg >> 3;
+  int64_t t = xcd < big ? xcd * per + i : big * per + (xcd - big) * (per - 1) + i;
+  const int64_t strip = 8 * tb;                         // strips of 8 row tiles
+  const int64_t s = t / strip, r = t - s * strip;
+  const int64_t h = ta - s * 8 < 8 ? ta - s * 8 : 8;
+  *a = s * 8 + r % h;
+  *b = r / h;
+}
+
+// Second best and position of the best in one float: the value rounded away from zero far enough (towards +inf) that the
+// low 7 bits are free.  Read as a float it is never below the value and at most 2^-15 of it above.
+__device__ __forceinline__ float pack_second(float second, int pos) {
+  u32 u = __float_as_uint(second);
+  if (u >> 31) u = u > 0x800000FFu ? (u & ~0x7Fu) - 0x80u : 0u;
+  else u = (u + 0x7Fu) & ~0x7Fu;
+  return __uint_as_float(u | (u32)pos);
+}
+
+struct Best { float m, second; int pos; };
+__device__ __forceinline__ Best join_best(Best a, Best b) {   // rows of a come before rows of b
+  Best o;
+  o.second = fmaxf(fminf(a.m, b.m), fmaxf(a.second, b.second));
+  o.pos = b.m > a.m ? b.pos : a.pos;
+  o.m = fmaxf(a.m, b.m);
+  return o;
+}
+// of lanes whose rows interleave: the smaller position among equal maxima
+__device__ __forceinline__ Best join_mixed(Best a, Best b) {
+  Best o;
+  o.second = fmaxf(fminf(a.m, b.m), fmaxf(a.second, b.second));
+  o.pos = b.m > a.m ? b.pos : (a.m > b.m ? a.pos : (a.pos < b.pos ? a.pos : b.pos));
+  o.m = fmaxf(a.m, b.m);
+  return o;
+}
+
+// The scores of a wavefront's tile in place of its products: s = acc * (row factor * query factor) + bias, -inf for
+// rows that do not exist (past the end, or bias -inf: whatever their products are).
+// rowdata: LDS, {row factor, bias} of the workgroup's 128 rows, filled here.
+__device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[2][2]) {
+  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1;
+  const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + kSmTile <= S.nx;   // (the same in the workgroup)
+  if (!plain) {
+    if (threadIdx.x < kSmTile) {
+      const int64_t j = a0 + threadIdx.x;
+      const bool in = j < S.nx;
+      rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+    const float cq = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] : 1.f);
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (plain) {
+          acc[ib][jb][r] *= cq;
+        } else {
+          const float2 rd = rowdata[wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)];
+          const float s = acc[ib][jb][r] * rd.x * cq + rd.y;
+          acc[ib][jb][r] = rd.y == neg_inf() ? neg_inf() : s;
+        }
+      }
+  }
+}
+
+// ---- forward: scores -> softmax records ---------------------------------------------
+// Bound by the matrix cores for long vectors and by the epilogue's exponentials (some 12 vector instructions per score)
+// for short ones; two workgroups per CU let one's epilogue run beside the other's products.
+template <int PLANES, bool BF16, bool SECOND>
+__global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords R, int64_t ta, int64_t tb) {
+  extern __shared__ __align__(16) char lds[];
+  int64_t ia, ib_;
+  tile_of(blockIdx.x, ta, tb, &ia, &ib_);
+  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
+  f32x16 acc[2][2] = {};
+  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kblocks, lds, acc);
+  float2* rowdata = reinterpret_cast<float2*>(lds);
+  finish_scores(S, a0, b0, rowdata, acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  float4* other = reinterpret_cast<float4*>(lds + 1024);            // [128] records of the second 64 rows
+  float* other_second = reinterpret_cast<float*>(lds + 1024 + 2048);
+  float mx[2], sum[2], ent[2];
+  Best best[2];
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    float m = neg_inf(), second = neg_inf();
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float s = acc[ib][jb][r];
+        if (SECOND) second = __builtin_amdgcn_fmed3f(s, m, second);
+        m = fmaxf(m, s);
+      }
+    int pos = 0;
+    if (SECOND) {
+#pragma unroll
+      for (int ib = 1; ib >= 0; --ib)
+#pragma unroll
+        for (int r = 15; r >= 0; --r)
+          pos = acc[ib][jb][r] == m ? wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half : pos;
+      Best mine{m, second, pos};
+      Best theirs{__shfl_xor(m, 32), __shfl_xor(second, 32), __shfl_xor(pos, 32)};
+      best[jb] = join_mixed(mine, theirs);
+      m = best[jb].m;
+    } else {
+      m = fmaxf(m, __shfl_xor(m, 32));
+    }
+    float l = 0.f, h = 0.f;
+    const float base = m > neg_inf() ? m : 0.f;
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) softmax_add(acc[ib][jb][r] - base, &l, &h);
+    l += __shfl_xor(l, 32);
+    h += __shfl_xor(h, 32);
+    mx[jb] = m; sum[jb] = l; ent[jb] = h;
+    if (R.keep) {
+      const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+      if (qi < S.nq)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const int64_t j = a0 + wa * 64 + ib * 32 + 8 * (r >> 2) + 4 * half;   // keep_ld is a multiple of 128: no tail
+            *reinterpret_cast<float4*>(R.keep + qi * R.keep_ld + j) =
+                make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
+          }
+    }
+  }
+  __syncthreads();                                                  // (rowdata has been read)
+  if (wa == 1 && half == 0) {
+#pragma unroll
+    for (int jb = 0; jb < 2; ++jb) {
+      const int c = wb * 64 + jb * 32 + (lane & 31);
+      other[c] = make_float4(mx[jb], sum[jb], ent[jb], SECOND ? __int_as_float(best[jb].pos) : 0.f);
+      if (SECOND) other_second[c] = best[jb].second;
+    }
+  }
+  __syncthreads();
+  if (wa == 0 && half == 0) {
+#pragma unroll
+    for (int jb = 0; jb < 2; ++jb) {
+      const int c = wb * 64 + jb * 32 + (lane & 31);
+      const int64_t qi = b0 + c;
+      if (qi >= S.nq) continue;
+      const float4 o = other[c];
+      const float m = fmaxf(mx[jb], o.x);
+      float l = 0.f, h = 0.f;
+      softmax_join(m, mx[jb], sum[jb], ent[jb], &l, &h);
+      softmax_join(m, o.x, o.y, o.z, &l, &h);
+      float w = 0.f;
+      if (SECOND) {
+        const Best b = join_best(best[jb], Best{o.x, other_second[c], __float_as_int(o.w)});
+        w = pack_second(b.second, b.pos);
+      }
+      R.rec[qi * R.parts + ia] = make_float4(m, l, h, w);
+    }
+  }
+}
+
+// ---- forward for few queries ----------------------------------------------------------
+// Up to 64 queries the rows are what there is to read: a wavefront loads fragments of 32 rows straight from memory
+// (no LDS, 16 bytes a lane and load) and multiplies them with all queries, whose fragments wait in LDS; four wavefronts
+// make the record of 128 rows.  fp32 rows use v_mfma_f32_16x16x4_f32: exact products, and its 157 TFLOP/s are far above
+// what the stream of rows can ask for.
+// In the 16x16 layouts a lane holds row lane & 15 of A, and of the result column lane & 15 and rows 4 (lane >> 4) + r.
+template <int DT>
+struct FewMul {
+  typedef typename Elem<DT>::T T;
+  static constexpr int KS = DT == 0 ? 16 : 32;        // K elements per step: 16 bytes for each of 4 lane groups
+  static constexpr int PER = DT == 0 ? 4 : 8;         // of them in a lane
+  static __device__ __forceinline__ f32x4 mul(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (DT == 0) {
+      const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+      return c;
+    } else if constexpr (DT == 1) {
+      return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    } else {
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+  }
+  // PER elements k .. of a row of d, zeros past its end
+  static __device__ __forceinline__ u32x4 load(const T* row, int k, int d) {
+    u32x4 v;
+    if (k + PER <= d) {
+      __builtin_memcpy(&v, row + k, 16);
+    } else {
+      T e[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) e[i] = k + i < d ? row[k + i] : (T)0.f;
+      __builtin_memcpy(&v, e, 16);
+    }
+    return v;
+  }
+};
+
+constexpr int kFewChunkBytes = 64 * 1024;             // of query fragments in LDS
+template <int DT, int NT>
+constexpr int few_chunk() { return kFewChunkBytes / (NT * 1024) * FewMul<DT>::KS; }   // K elements of a chunk
+
+template <int DT, int NT, bool SECOND>
+__global__ __launch_bounds__(256) void sm_scores_few_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t nb,
+                                                            const typename Elem<DT>::T* __restrict__ q, int nq, int d,
+                                                            float scale, const float* __restrict__ bias, SmRecords R) {
+  typedef FewMul<DT> F;
+  constexpr int CH = few_chunk<DT, NT>();
+  extern __shared__ __align__(16) char lds[];
+  u32x4* frag = reinterpret_cast<u32x4*>(lds);        // [step][NT][64]
+  const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4;
+  const int64_t part = blockIdx.x, j0 = part * kSmRecRows + wave * 32;
+  const typename F::T* row[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int64_t j = j0 + i * 16 + (lane & 15);
+    row[i] = x + (j < nb ? j : nb - 1) * d;
+  }
+  f32x4 acc[2][NT] = {};
+  for (int c0 = 0; c0 < d; c0 += CH) {
+    const int c1 = c0 + CH < d ? c0 + CH : d, steps = (c1 - c0 + F::KS - 1) / F::KS;
+    if (c0 > 0) __syncthreads();
+    for (int i = threadIdx.x; i < steps * NT * 64; i += 256) {
+      const int l = i & 63, t = (i >> 6) % NT, s = (i >> 6) / NT, qi = t * 16 + (l & 15);
+      u32x4 v = {0, 0, 0, 0};
+      if (qi < nq) v = F::load(q + (int64_t)qi * d, c0 + s * F::KS + (l >> 4) * F::PER, d);
+      frag[i] = v;
+    }
+    __syncthreads();
+    constexpr int U = 8;
+    int s = 0;
+    for (; s + U <= steps && c0 + (s + U) * F::KS <= d; s += U) {
+      u32x4 a[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) __builtin_memcpy(&a[u][i], row[i] + c0 + (s + u) * F::KS + g * F::PER, 16);
+      __builtin_amdgcn_sched_barrier(0);              // (all sixteen loads leave before the first is waited for)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const u32x4 b = frag[((s + u) * NT + t) * 64 + lane];
+          acc[0][t] = F::mul(a[u][0], b, acc[0][t]);
+          acc[1][t] = F::mul(a[u][1], b, acc[1][t]);
+        }
+      settle_products();
+    }
+    for (; s < steps; ++s) {
+      const int k = c0 + s * F::KS + g * F::PER;
+      const u32x4 a0 = F::load(row[0], k, d), a1 = F::load(row[1], k, d);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const u32x4 b = frag[(s * NT + t) * 64 + lane];
+        acc[0][t] = F::mul(a0, b, acc[0][t]);
+        acc[1][t] = F::mul(a1, b, acc[1][t]);
+      }
+      settle_products();
+    }
+  }
+  __syncthreads();
+  float4* recs = reinterpret_cast<float4*>(lds);                   // [4][NT * 16]
+  float* seconds = reinterpret_cast<float*>(lds + 4 * NT * 16 * 16);
+  float bj[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t j = j0 + i * 16 + 4 * g + r;
+      bj[i][r] = j < nb ? (bias ? bias[j] : 0.f) : neg_inf();
+    }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float m = neg_inf(), second = neg_inf();
+    float s[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float v = acc[i][t][r] * scale + bj[i][r];
+        s[i][r] = bj[i][r] == neg_inf() ? neg_inf() : v;
+        if (SECOND) second = __builtin_amdgcn_fmed3f(s[i][r], m, second);
+        m = fmaxf(m, s[i][r]);
+      }
+    const int qi = t * 16 + (lane & 15);
+    if (R.keep && qi < nq)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<float4*>(R.keep + (int64_t)qi * R.keep_ld + j0 + i * 16 + 4 * g) =
+            make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
+    Best b{m, second, 0};
+    if (SECOND) {
+#pragma unroll
+      for (int i = 1; i >= 0; --i)
+#pragma unroll
+        for (int r = 3; r >= 0; --r) b.pos = s[i][r] == m ? wave * 32 + i * 16 + 4 * g + r : b.pos;
+    }
+#pragma unroll
+    for (int w = 16; w <= 32; w <<= 1) {
+      if (SECOND) b = join_mixed(b, Best{__shfl_xor(b.m, w), __shfl_xor(b.second, w), __shfl_xor(b.pos, w)});
+      else b.m = fmaxf(b.m, __shfl_xor(b.m, w));
+    }
+    float l = 0.f, h = 0.f;
+    const float base = b.m > neg_inf() ? b.m : 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) softmax_add(s[i][r] - base, &l, &h);
+#pragma unroll
+    for (int w = 16; w <= 32; w <<= 1) { l += __shfl_xor(l, w); h += __shfl_xor(h, w); }
+    if (g == 0) {
+      recs[wave * NT * 16 + qi] = make_float4(b.m, l, h, __int_as_float(b.pos));
+      seconds[wave * NT * 16 + qi] = b.second;
+    }
+  }
+  __syncthreads();
+  const int qi = threadIdx.x;
+  if (qi >= nq || qi >= NT * 16) return;
+  Best b{neg_inf(), neg_inf(), 0};
+  for (int w = 0; w < 4; ++w) {
+    const float4 o = recs[w * NT * 16 + qi];
+    b = join_best(b, Best{o.x, seconds[w * NT * 16 + qi], __float_as_int(o.w)});
+  }
+  float l = 0.f, h = 0.f;
+  for (int w = 0; w < 4; ++w) {
+    const float4 o = recs[w * NT * 16 + qi];
+    softmax_join(b.m, o.x, o.y, o.z, &l, &h);
+  }
+  R.rec[(int64_t)qi * R.parts + part] = make_float4(b.m, l, h, SECOND ? pack_second(b.second, b.pos) : 0.f);
+}
+
+// ---- finish: records -> normaliser, entropy, targets, alternatives ------------------------
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) v = fmaxf(v, __shfl_xor(v, w));
+  return v;
+}
+
+// <q, x_j> for eight rows at once, eight lanes a row; every lane of a row's group gets the sum
+template <typename T>
+__device__ __forceinline__ float dot_8_rows(const T* __restrict__ q, const T* __restrict__ row, int d) {
+  constexpr int V = 16 / sizeof(T);
+  const int l = lane_id() & 7;
+  float acc = 0.f;
+  int k = l * V;
+  for (; k + V <= d; k += 8 * V) {
+    T a[V], b[V];
+    __builtin_memcpy(a, q + k, 16);
+    __builtin_memcpy(b, row + k, 16);
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc = __builtin_fmaf(to_f32(a[i]), to_f32(b[i]), acc);
+  }
+  for (int i = k; i < d && i < k + V; ++i) acc = __builtin_fmaf(to_f32(q[i]), to_f32(row[i]), acc);
+  acc += __shfl_xor(acc, 1);
+  acc += __shfl_xor(acc, 2);
+  acc += __shfl_xor(acc, 4);
+  return acc;
+}
+
+// One workgroup per query.  The k best rows lie in the k records with the best maxima (a row outside them is beaten by k
+// maxima; records cover consecutive rows, so ties fall to the smaller row as well).  Of such a record only the maximum
+// can count unless its second best reaches the k-th best maximum: then its 128 scores are computed again in fp32.
+// Where that would be common (few records, or many alternatives) the scores have been kept, and are read instead.
+template <int DT>
+__global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R) {
+  typedef typename Elem<DT>::T T;
+  constexpr int TOT = 128;
+  __shared__ u64 slots[4 * TOT];
+  __shared__ u64 chosen[VS_MAX_TOP];
+  __shared__ u64 shared_bound;
+  __shared__ float red[3][4];
+  const int64_t qi = blockIdx.x;
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const float4* rec = R.rec + qi * R.parts;
+  float m = neg_inf();
+  for (int64_t p = threadIdx.x; p < R.parts; p += 256) m = fmaxf(m, rec[p].x);
+  m = wave_max(m);
+  if (lane == 0) red[0][wave] = m;
+  if (threadIdx.x == 0) shared_bound = KEY_EMPTY;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  float l = 0.f, h = 0.f;
+  for (int64_t p = threadIdx.x; p < R.parts; p += 256) {
+    const float4 r = rec[p];
+    softmax_join(m, r.x, r.y, r.z, &l, &h);
+  }
+  l = wave_sum(l);
+  h = wave_sum(h);
+  if (lane == 0) { red[1][wave] = l; red[2][wave] = h; }
+  __syncthreads();
+  l = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  h = red[2][0] + red[2][1] + red[2][2] + red[2][3];
+  const bool empty = m == neg_inf() && l == 0.f;
+  const float logl = empty ? 0.f : logf(l), lse = empty ? neg_inf() : m + logl;
+  if (threadIdx.x == 0) {
+    F.lse[qi] = lse;
+    F.entropy[qi] = empty ? 0.f : logl - h / l;
+  }
+  const T* x = static_cast<const T*>(F.x);
+  const T* q = static_cast<const T*>(F.q) + qi * F.d;
+  const int group = lane >> 3;
+  for (int t0 = wave * 8; t0 < F.nt; t0 += 32) {
+    const int t = t0 + group;
+    const int64_t j = t < F.nt ? F.targets[qi * F.nt + t] : -1;
+    const bool in = j >= 0 && j < F.nb;
+    const float b = in && F.bias ? F.bias[j] : 0.f;
+    const float s = dot_8_rows(q, x + (in ? j : 0) * F.d, F.nb > 0 ? F.d : 0) * F.scale + b;
+    if ((lane & 7) == 0 && t < F.nt)
+      F.logp[qi * F.nt + t] = !in ? 0.f : (b == neg_inf() ? neg_inf() : s - lse);
+  }
+  if (F.k == 0) return;
+  WaveSelect<2> sel;
+  auto start = [&]() {
+    sel.init(slots + wave * TOT, TOT, F.k, &shared_bound);
+    sel.set_metric(1);
+  };
+  if (R.keep) {
+    start();
+    const float* s = R.keep + qi * R.keep_ld;
+    for (int64_t j0 = wave * 64; j0 < F.nb; j0 += 256) {
+      const int64_t j = j0 + lane;
+      const float v = j < F.nb ? s[j] : neg_inf();
+      sel.push_value(v > neg_inf(), v, (u32)j);
+    }
+  } else {
+    start();
+    for (int64_t p0 = wave * 64; p0 < R.parts; p0 += 256) {
+      const int64_t p = p0 + lane;
+      const float v = p < R.parts ? rec[p].x : neg_inf();
+      sel.push_value(v > neg_inf(), v, (u32)p);
+    }
+    sel.finish();
+    __syncthreads();
+    KeySink to{chosen, nullptr, nullptr, nullptr, nullptr, 1};
+    block_rank_merge(slots, TOT, 4, F.k, to, 0);
+    if (threadIdx.x == 0) shared_bound = KEY_EMPTY;
+    __syncthreads();
+    const u64 last = chosen[F.k - 1];
+    const float tau = last == KEY_EMPTY ? neg_inf() : key_value(last, 1);
+    start();
+    for (int c0 = 0; c0 < F.k; c0 += 64) {
+      const int c = c0 + lane;
+      const u64 key = c < F.k ? chosen[c] : KEY_EMPTY;
+      const u32 p = key_index(key);
+      const float w = key != KEY_EMPTY ? rec[p].w : 0.f;
+      const bool whole = key != KEY_EMPTY && w >= tau;
+      if (wave == 0) {                                      // the maximum alone
+        const u32 j = p * kSmRecRows + (__float_as_uint(w) & 127u);
+        sel.push(key != KEY_EMPTY && !whole, make_key(key_value(key, 1), j, 1));
+      }
+      for (u64 todo = __ballot(whole); todo; todo &= todo - 1) {
+        const u32 pw = __shfl(p, __ffsll(todo) - 1);
+        for (int r0 = wave * 8; r0 < kSmRecRows; r0 += 32) {
+          const int64_t j = (int64_t)pw * kSmRecRows + r0 + group;
+          const bool in = j < F.nb;
+          const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
+          const float s = dot_8_rows(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b;
+          sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
+        }
+      }
+    }
+  }
+  sel.finish();
+  __syncthreads();
+  KeySink to{chosen, nullptr, nullptr, nullptr, nullptr, 1};
+  block_rank_merge(slots, TOT, 4, F.k, to, 0);
+  __syncthreads();
+  if ((int)threadIdx.x < F.k) {
+    const u64 key = chosen[threadIdx.x];
+    F.top_logp[qi * F.k + threadIdx.x] = key == KEY_EMPTY ? neg_inf() : key_value(key, 1) - lse;
+    F.top_ids[qi * F.k + threadIdx.x] = key == KEY_EMPTY ? -1 : (int64_t)key_index(key);
+  }
+}
+
+// ---- preparation of operands ------------------------------------------------------------
+// The power of two that brings a largest component of `mx` into [128, 256); what lies 2^22 below it still has its head's
+// full 11 bits, and a tail keeps 2^-32 of the largest component.
+__device__ __forceinline__ void row_scale(float mx, float* up, float* down) {
+  int e = mx > 0.f && mx < __builtin_inff() ? 8 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
+  e = e < -120 ? -120 : (e > 120 ? 120 : e);
+  *up = __builtin_ldexpf(1.f, e);
+  *down = __builtin_ldexpf(1.f, -e);
+}
+// element v (scaled) at position k of a row of K blocks
+template <int PLANES>
+__device__ __forceinline__ void put_planes(char* row, int64_t k, float v) {
+  const _Float16 hi = (_Float16)v;
+  if (PLANES == 1) {
+    reinterpret_cast<_Float16*>(row)[k] = hi;
+  } else {
+    _Float16* b = reinterpret_cast<_Float16*>(row + (k >> 5) * 128) + (k & 31);
+    b[0] = hi;
+    b[32] = (_Float16)(v - (float)hi);
+  }
+}
+
+template <int DT, int PLANES>
+__global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
+                                                           int64_t dp, const float* __restrict__ bias,
+                                                           char* __restrict__ planes, float* __restrict__ scale) {
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= n) return;
+  const int lane = lane_id();
+  const typename Elem<DT>::T* row = x + r * d;
+  const bool gone = bias && bias[r] == neg_inf();
+  float mx = 0.f;
+  if (!gone)
+    for (int k = lane; k < d; k += 64) mx = fmaxf(mx, fabsf(to_f32(row[k])));
+  mx = wave_max(mx);
+  float up, down;
+  row_scale(mx, &up, &down);
+  char* out = planes + r * (dp * 2 * PLANES);
+  for (int k = lane; k < dp; k += 64) put_planes<PLANES>(out, k, k < d && !gone ? to_f32(row[k]) * up : 0.f);
+  if (lane == 0) scale[r] = down;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void sm_colmax_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
+                                                        const float* __restrict__ bias, const float* __restrict__ factor,
+                                                        int64_t rows_per, u32* __restrict__ colmax) {
+  const int t = blockIdx.x * 64 + (threadIdx.x & 63);
+  const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < n ? r0 + rows_per : n;
+  float mx = 0.f;
+  if (t < d)
+    for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+      const float f = bias && bias[r] == neg_inf() ? 0.f : (factor ? factor[r] : 1.f);
+      if (f != 0.f) mx = fmaxf(mx, fabsf(to_f32(x[r * d + t])) * f);
+    }
+  // (a maximum does not depend on the order; non-negative floats are ordered as their bits)
+  if (t < d && mx > 0.f) atomicMax(colmax + t, __float_as_uint(mx));
+}
+
+// 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r
+template <int DT, int PLANES>
+__global__ __launch_bounds__(256) void sm_prep_cols_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
+                                                           int64_t np, const float* __restrict__ bias,
+                                                           const float* __restrict__ factor, const u32* __restrict__ colmax,
+                                                           char* __restrict__ planes, float* __restrict__ scale) {
+  __shared__ float tile[64][65];
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const int t0 = blockIdx.y * 64, lane = lane_id(), wave = threadIdx.x >> 6;
+  for (int i = wave; i < 64; i += 4) {
+    const int64_t r = r0 + i;
+    float v = 0.f;
+    if (r < n && t0 + lane < d) {
+      const float f = bias && bias[r] == neg_inf() ? 0.f : (factor ? factor[r] : 1.f);
+      if (f != 0.f) v = to_f32(x[r * d + t0 + lane]) * f;          // (what takes no part is not read)
+    }
+    tile[i][lane] = v;
+  }
+  __syncthreads();
+  for (int i = wave; i < 64; i += 4) {
+    const int t = t0 + i;
+    if (t >= d) break;
+    float up, down;
+    row_scale(__uint_as_float(colmax[t]), &up, &down);
+    if (r0 + lane < np) put_planes<PLANES>(planes + (int64_t)t * (np * 2 * PLANES), r0 + lane, tile[lane][i] * up);
+    if (blockIdx.x == 0 && lane == 0) scale[t] = down;
+  }
+}
+
+// ---- backward ------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, int64_t nb, float4* __restrict__ coef,
+                                                       float* __restrict__ bound) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= nq) return;
+  float sum = 0.f, mag = 0.f;
+  if (g.g_logp)
+    for (int t = 0; t < g.nt; ++t) {
+      const int64_t j = g.targets[i * g.nt + t];
+      if (j < 0 || j >= nb) continue;
+      const float v = g.g_logp[i * g.nt + t];
+      sum += v;
+      mag += fabsf(v);
+    }
+  const float c = (g.g_lse ? g.g_lse[i] : 0.f) - sum;
+  const float ge = g.g_entropy ? g.g_entropy[i] : 0.f, ent = g.g_entropy ? g.entropy[i] : 0.f;
+  // |G| <= |c| p + |g_entropy| (p |logp| + p H) + sum |g_logp|, and p |logp| <= 1 / e
+  const float top = fabsf(c) + mag + fabsf(ge) * (0.37f + fabsf(ent));
+  int e = top > 0.f && top < __builtin_inff() ? (int)__builtin_amdgcn_frexp_expf(top) : 0;
+  e = e < -100 ? -100 : e;
+  // (infinite or NaN: so are the row's gradients; 0, a padded query: it takes no part, whatever it holds)
+  bound[i] = top == 0.f || !(top < __builtin_inff()) ? top : __builtin_ldexpf(1.f, e);
+  coef[i] = make_float4(c, ge, ent, top == 0.f ? neg_inf() : g.lse[i]);
+}
+
+// Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
+// G / bound 2^14 in fp16: a value keeps 11 bits (22 with a tail) down to 2^-28 of the bound and 2^-38 of it below.
+template <int PLANES, bool BF16>
+__global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut O, int64_t ta, int64_t tb) {
+  extern __shared__ __align__(16) char lds[];
+  int64_t ia, ib_;
+  tile_of(blockIdx.x, ta, tb, &ia, &ib_);
+  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
+  f32x16 acc[2][2] = {};
+  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kblocks, lds, acc);
+  finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+    const bool in = qi < S.nq;
+    const float4 c = in ? O.coef[qi] : make_float4(0.f, 0.f, 0.f, neg_inf());
+    const bool some = c.w != neg_inf();
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float s = acc[ib][jb][r];
+        const float logp = s - c.w;
+        const float v = exp_neg(logp) * (c.x - c.y * (fmaxf(logp, -1000.f) + c.z));
+        // a row that does not exist carries the mark of its score until the targets are in
+        acc[ib][jb][r] = s == neg_inf() || !some ? neg_inf() : v;
+      }
+    if (O.g_logp && in)
+      for (int t = 0; t < O.nt; ++t) {
+        const int64_t j = O.targets[qi * O.nt + t] - O.row0 - a0 - wa * 64;   // relative to the wavefront's rows
+        if (j >= 0 && j < 64) {
+          const float gl = O.g_logp[qi * O.nt + t];
+#pragma unroll
+          for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if ((int)j == ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) acc[ib][jb][r] += gl;
+        }
+      }
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[ib][jb][r] = acc[ib][jb][r] == neg_inf() ? 0.f : acc[ib][jb][r];
+  }
+  __syncthreads();                                                  // (rowdata has been read)
+  if (O.db) {                                                       // column sums of this tile, in a fixed order
+    float* dbs = reinterpret_cast<float*>(lds);                     // [2][128]
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float v = acc[ib][0][r] + acc[ib][1][r];
+        v += __uint_as_float(lane_xor_u32<1>(__float_as_uint(v)));
+        v += __uint_as_float(lane_xor_u32<2>(__float_as_uint(v)));
+        v += __uint_as_float(lane_xor_u32<4>(__float_as_uint(v)));
+        v += __uint_as_float(lane_xor_u32<8>(__float_as_uint(v)));
+        v += __shfl_xor(v, 16);
+        if ((lane & 31) == 0) dbs[wb * 128 + wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half] = v;
+      }
+    __syncthreads();
+    if (threadIdx.x < 128 && a0 + threadIdx.x < S.nx)
+      O.db[ib_ * O.db_ld + a0 + threadIdx.x] = dbs[threadIdx.x] + dbs[128 + threadIdx.x];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+    const float bnd = qi < S.nq ? O.bound[qi] : 0.f;
+    const float inv = bnd == 0.f ? 0.f : 16384.f / bnd;
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[ib][jb][r] *= inv;
+  }
+  constexpr int LD = 2 * kSmTile + 16;                              // bytes of a row of the staged tile
+  constexpr int PER = PLANES == 2 ? 32 : 64;                        // elements of a K block
+  for (int plane = 0; plane < PLANES; ++plane) {
+    if (O.g) {
+      // rows of G: queries; four consecutive rows of x are 8 bytes of it
+#pragma unroll
+      for (int jb = 0; jb < 2; ++jb)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            f16x4 v;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = (_Float16)acc[ib][jb][r + u];
+            *reinterpret_cast<f16x4*>(lds + (wb * 64 + jb * 32 + (lane & 31)) * LD +
+                                      2 * (wa * 64 + ib * 32 + 2 * r + 4 * half)) = v;
+          }
+      __syncthreads();
+      for (int i = threadIdx.x; i < kSmTile * 16; i += 256) {
+        const int row = i >> 4, k = (i & 15) * 8;                   // 8 elements
+        if (b0 + row < S.nq)
+          *reinterpret_cast<u32x4*>(static_cast<char*>(O.g) + (b0 + row) * O.g_row_bytes + (a0 + k) / PER * 128 + plane * 64 +
+                                    (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+      }
+      __syncthreads();
+    }
+    if (O.gt) {
+#pragma unroll
+      for (int jb = 0; jb < 2; ++jb)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            *reinterpret_cast<_Float16*>(lds + (wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) * LD +
+                                         2 * (wb * 64 + jb * 32 + (lane & 31))) = (_Float16)acc[ib][jb][r];
+      __syncthreads();
+      for (int i = threadIdx.x; i < kSmTile * 16; i += 256) {
+        const int row = i >> 4, k = (i & 15) * 8;
+        if (a0 + row < S.nx)
+          *reinterpret_cast<u32x4*>(static_cast<char*>(O.gt) + (a0 + row) * O.gt_row_bytes + (b0 + k) / PER * 128 + plane * 64 +
+                                    (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+      }
+      __syncthreads();
+    }
+    if (PLANES == 2 && plane == 0) {
+#pragma unroll
+      for (int jb = 0; jb < 2; ++jb)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[ib][jb][r] -= (float)(_Float16)acc[ib][jb][r];
+    }
+  }
+}
+
+template <int PLANES>
+__global__ __launch_bounds__(256, 2) void sm_product_kernel(SmMatrix A, SmMatrix B, int64_t kblocks, int splits, int add,
+                                                            float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb) {
+  extern __shared__ __align__(16) char lds[];
+  int64_t ia, ib_;
+  const int64_t tiles = ta * tb;
+  const int split = (int)(blockIdx.x / tiles);
+  tile_of(blockIdx.x - split * tiles, ta, tb, &ia, &ib_);
+  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
+  const int64_t k0 = kblocks * split / splits, k1 = kblocks * (split + 1) / splits;
+  f32x16 acc[2][2] = {};
+  if (k1 > k0) TileMul<PLANES, false>::run(A, a0, B, b0, k0, k1, lds, acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
+    if (b >= B.rows) continue;
+    float* out = part + (split * B.rows + b) * ld;
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int64_t a = a0 + wa * 64 + ib * 32 + 2 * r + 4 * half;
+        if (a >= ld) continue;                                      // (ld is a multiple of 4 and at least A.rows)
+        float4 v = make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
+        float4* o = reinterpret_cast<float4*>(out + a);
+        if (add) { const float4 w = *o; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+        *o = v;
+      }
+  }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void sm_product_out_kernel(const float* __restrict__ part, int splits, int64_t rows,
+                                                             int64_t ld, int d, const float* __restrict__ sa,
+                                                             const float* __restrict__ sb, float alpha,
+                                                             typename Elem<DT>::T* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * d) return;
+  const int64_t b = i / d;
+  const int a = (int)(i - b * d);
+  float v = 0.f;
+  for (int s = 0; s < splits; ++s) v += part[(s * rows + b) * ld + a];
+  // (powers of two first: the product with alpha is the only rounding before the last)
+  v = v * sa[a] * (sb ? sb[b] : 1.f);
+  out[i] = (typename Elem<DT>::T)(v * alpha);
+}
+
+__global__ __launch_bounds__(256) void sm_sum_parts_kernel(const float* __restrict__ part, int64_t parts, int64_t ld,
+                                                           int64_t n, float* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float v = 0.f;
+  for (int64_t p = 0; p < parts; ++p) v += part[p * ld + i];
+  out[i] = v;
+}
+
+__global__ __launch_bounds__(256) void sm_zero_kernel(u32* __restrict__ p, int64_t words) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+__global__ __launch_bounds__(64) void sm_zero_bytes_kernel(unsigned char* __restrict__ p, int n) {
+  if ((int)threadIdx.x < n) p[threadIdx.x] = 0;
+}
+
+inline int64_t tiles(int64_t n) { return (n + kSmTile - 1) / kSmTile; }
+inline unsigned grid_of(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
+
+}  // namespace
+
+void launch_sm_zero(void* p, int64_t bytes, hipStream_t st) {
+  const int64_t words = bytes / 4;
+  if (words > 0) {
+    const unsigned g = grid_of(words, 256);
+    sm_zero_kernel<<<g < 4096u ? g : 4096u, 256, 0, st>>>(static_cast<u32*>(p), words);
+  }
+  if (bytes & 3) sm_zero_bytes_kernel<<<1, 64, 0, st>>>(static_cast<unsigned char*>(p) + words * 4, (int)(bytes & 3));
+}
+
+void launch_sm_prep_rows(const SmForm& f, const void* x, int64_t n, int d, const float* bias, void* planes, float* scale,
+                         hipStream_t st) {
+  if (n == 0) return;
+  const int64_t dp = f.blocks(d) * f.per_block();
+  const unsigned g = grid_of(n, 4);
+  if (f.dtype == 0)
+    sm_prep_rows_kernel<0, 2><<<g, 256, 0, st>>>(static_cast<const float*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
+  else if (f.dtype == 1)
+    sm_prep_rows_kernel<1, 1><<<g, 256, 0, st>>>(static_cast<const _Float16*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
+  else
+    sm_prep_rows_kernel<2, 1><<<g, 256, 0, st>>>(static_cast<const __bf16*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
+}
+
+namespace {
+template <int DT, int PLANES>
+void prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor, u32* colmax,
+               void* planes, float* scale, hipStream_t st) {
+  typedef typename Elem<DT>::T T;
+  const int64_t np = f.blocks(n) * f.per_block();
+  const unsigned gy = (unsigned)(n < 64 * 256 ? (n + 63) / 64 : 256);
+  const int64_t per = (n + gy - 1) / gy;
+  launch_sm_zero(colmax, (int64_t)d * 4, st);
+  sm_colmax_kernel<DT><<<dim3(grid_of(d, 64), gy), 256, 0, st>>>(static_cast<const T*>(x), n, d, bias, factor, per, colmax);
+  sm_prep_cols_kernel<DT, PLANES><<<dim3(grid_of(np, 64), grid_of(d, 64)), 256, 0, st>>>(
+      static_cast<const T*>(x), n, d, np, bias, factor, colmax, static_cast<char*>(planes), scale);
+}
+}  // namespace
+
+void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor,
+                         u32* colmax, void* planes, float* scale, hipStream_t st) {
+  if (n == 0) return;
+  if (f.dtype == 0) prep_cols<0, 2>(f, x, n, d, bias, factor, colmax, planes, scale, st);
+  else if (f.dtype == 1) prep_cols<1, 1>(f, x, n, d, bias, factor, colmax, planes, scale, st);
+  else prep_cols<2, 1>(f, x, n, d, bias, factor, colmax, planes, scale, st);
+}
+
+void launch_sm_scores(const SmForm& f, bool direct, const SmScores& s, const SmRecords& r, bool second, hipStream_t st) {
+  const int64_t ta = tiles(s.nx), tb = tiles(s.nq);
+  const unsigned g = (unsigned)(ta * tb);
+  auto run = [&](auto kern) { kern<<<g, 256, kTileLds, st>>>(s, r, ta, tb); };
+  if (f.planes == 2) { if (second) run(sm_scores_kernel<2, false, true>); else run(sm_scores_kernel<2, false, false>); }
+  else if (direct && f.dtype == 2) { if (second) run(sm_scores_kernel<1, true, true>); else run(sm_scores_kernel<1, true, false>); }
+  else { if (second) run(sm_scores_kernel<1, false, true>); else run(sm_scores_kernel<1, false, false>); }
+}
+
+namespace {
+template <int DT, int NT>
+void scores_few(const void* x, int64_t nb, const void* q, int64_t nq, int d, float scale, const float* bias,
+                const SmRecords& r, bool second, hipStream_t st) {
+  typedef typename Elem<DT>::T T;
+  const unsigned g = grid_of(nb, kSmRecRows);
+  const int chunk = few_chunk<DT, NT>(), steps = ((d < chunk ? d : chunk) + FewMul<DT>::KS - 1) / FewMul<DT>::KS;
+  const int recs = 4 * NT * 16 * 20, frags = steps * NT * 1024, lds = frags > recs ? frags : recs;
+  if (second)
+    sm_scores_few_kernel<DT, NT, true><<<g, 256, lds, st>>>(static_cast<const T*>(x), nb, static_cast<const T*>(q), (int)nq, d, scale, bias, r);
+  else
+    sm_scores_few_kernel<DT, NT, false><<<g, 256, lds, st>>>(static_cast<const T*>(x), nb, static_cast<const T*>(q), (int)nq, d, scale, bias, r);
+}
+}  // namespace
+
+void launch_sm_scores_few(int dtype, const void* x, int64_t nb, const void* q, int64_t nq, int d, float scale,
+                          const float* bias, const SmRecords& r, bool second, hipStream_t st) {
+  if (nb == 0) return;
+#define FEW(DT)                                                                          \
+  do {                                                                                   \
+    if (nq <= 16) scores_few<DT, 1>(x, nb, q, nq, d, scale, bias, r, second, st);        \
+    else if (nq <= 32) scores_few<DT, 2>(x, nb, q, nq, d, scale, bias, r, second, st);   \
+    else scores_few<DT, 4>(x, nb, q, nq, d, scale, bias, r, second, st);                 \
+  } while (0)
+  if (dtype == 0) FEW(0);
+  else if (dtype == 1) FEW(1);
+  else FEW(2);
+#undef FEW
+}
+
+void launch_sm_finish(const SmFinish& f, const SmRecords& r, hipStream_t st) {
+  const unsigned g = (unsigned)f.nq;
+  if (f.dtype == 0) sm_finish_kernel<0><<<g, 256, 0, st>>>(f, r);
+  else if (f.dtype == 1) sm_finish_kernel<1><<<g, 256, 0, st>>>(f, r);
+  else sm_finish_kernel<2><<<g, 256, 0, st>>>(f, r);
+}
+
+void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, hipStream_t st) {
+  sm_coefs_kernel<<<grid_of(nq, 256), 256, 0, st>>>(g, nq, nb, coef, bound);
+}
+
+void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st) {
+  const int64_t ta = tiles(s.nx), tb = tiles(s.nq);
+  const unsigned g = (unsigned)(ta * tb);
+  if (f.planes == 2) sm_gradients_kernel<2, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
+  else if (direct && f.dtype == 2) sm_gradients_kernel<1, true><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
+  else sm_gradients_kernel<1, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
+}
+
+void launch_sm_product(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, int splits, bool add,
+                       float* part, int64_t ld, hipStream_t st) {
+  const int64_t ta = tiles(A.rows), tb = tiles(B.rows);
+  const unsigned g = (unsigned)(ta * tb * splits);
+  if (f.planes == 2) sm_product_kernel<2><<<g, 256, kTileLds, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
+  else sm_product_kernel<1><<<g, 256, kTileLds, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
+}
+
+void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* sa, const float* sb,
+                           float alpha, int dtype, void* out, hipStream_t st) {
+  const unsigned g = grid_of(rows * d, 256);
+  if (dtype == 0) sm_product_out_kernel<0><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<float*>(out));
+  else if (dtype == 1) sm_product_out_kernel<1><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<_Float16*>(out));
+  else sm_product_out_kernel<2><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<__bf16*>(out));
+}
+
+void launch_sm_sum_parts(const float* part, int64_t n_parts, int64_t ld, int64_t n, float* out, hipStream_t st) {
+  sm_sum_parts_kernel<<<grid_of(n, 256), 256, 0, st>>>(part, n_parts, ld, n, out);
+}

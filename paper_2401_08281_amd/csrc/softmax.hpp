@@ -1,0 +1,99 @@
+// Host-side declarations shared by the translation units of libvs_softmax.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "internal.hpp"
+#include "store.hpp"
+
+// ---- log-probabilities over rows (kernels_logprob.hip) ---------------------------
+// A matrix as the matrix cores read it: rows of whole 128-byte K blocks, `rows` of them that exist.  A K block holds
+// 64 fp16 or bf16 elements, or (planes == 2) 32 fp16 heads and behind them their 32 fp16 tails.  scale: factor of every
+// row (a power of two), or null (ones).
+struct SmMatrix {
+  const void* p = nullptr;
+  int64_t row_bytes = 0;
+  int64_t rows = 0;
+  const float* scale = nullptr;
+};
+constexpr int kSmTile = 128;        // rows of either operand that a workgroup takes
+constexpr int kSmRecRows = 128;     // rows that a softmax record covers
+constexpr int kSmFewQueries = 64;   // up to here the rows are streamed past all queries
+
+struct SmForm {                     // how the rows of a type are multiplied
+  int dtype, planes;                // planes 2: fp32 as head and tail
+  int per_block() const { return planes == 2 ? 32 : 64; }
+  int64_t blocks(int64_t k) const { return (k + per_block() - 1) / per_block(); }
+};
+
+// planes[r] <- the row as K blocks of fp16 parts times 1 / scale[r], the largest component in [128, 256); rows whose
+// bias is -inf become zeros.
+void launch_sm_prep_rows(const SmForm& f, const void* x, int64_t n, int d, const float* bias, void* planes,
+                         float* scale, hipStream_t st);
+// planes[t] <- column t of (factor[r] x[r]) as K blocks over r, times 1 / scale[t]; colmax: [d] u32 of scratch
+void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor,
+                         u32* colmax, void* planes, float* scale, hipStream_t st);
+
+struct SmScores {                   // s = scale <q, x> + bias for rows x0 .. x0 + nx of x
+  SmMatrix x, q;
+  int64_t kblocks = 0;              // K blocks of a row
+  int64_t nx = 0, nq = 0;
+  const float* bias = nullptr;      // of these rows
+  float scale = 1.f;
+};
+struct SmRecords {                  // softmax of 128 rows: {max, sum, sum e (s - max), second best | position of the max}
+  float4* rec = nullptr;            // [nq, parts]
+  int64_t parts = 0;
+  float* keep = nullptr;            // [nq, keep_ld] the scores themselves, or null
+  int64_t keep_ld = 0;
+};
+void launch_sm_scores(const SmForm& f, bool direct, const SmScores& s, const SmRecords& r, bool second, hipStream_t st);
+void launch_sm_scores_few(int dtype, const void* x, int64_t nb, const void* q, int64_t nq, int d, float scale,
+                          const float* bias, const SmRecords& r, bool second, hipStream_t st);
+struct SmFinish {
+  const void* x; int64_t nb; const void* q; int64_t nq; int d, dtype; float scale; const float* bias;
+  const int64_t* targets; int nt, k;
+  float* logp; float* lse; float* entropy; float* top_logp; int64_t* top_ids;
+};
+void launch_sm_finish(const SmFinish& f, const SmRecords& r, hipStream_t st);
+
+// backward
+struct SmGrads {
+  const float* lse; const float* entropy; const int64_t* targets; int nt;
+  const float* g_logp; const float* g_lse; const float* g_entropy;
+};
+// coef[i] = {coefficient of p, g_entropy, entropy, lse}, bound[i]: a power of two that no |G_ij| exceeds
+void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, hipStream_t st);
+struct SmGOut {
+  const float4* coef; const float* bound; const int64_t* targets; int nt; const float* g_logp; int64_t row0;
+  void* g; int64_t g_row_bytes;     // [nq][K blocks over the rows], or null
+  void* gt; int64_t gt_row_bytes;   // [nx][K blocks over the queries], or null
+  float* db; int64_t db_ld;         // [query tiles, db_ld] partial column sums, or null
+};
+void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st);
+// out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over `splits` workgroups: part[split][b][ld]
+void launch_sm_product(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, int splits, bool add,
+                       float* part, int64_t ld, hipStream_t st);
+// out[b][a] = alpha scale_a[a] scale_b[b] sum_split part[split][b][a]
+void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* scale_a,
+                           const float* scale_b, float alpha, int dtype, void* out, hipStream_t st);
+void launch_sm_sum_parts(const float* part, int64_t n_parts, int64_t ld, int64_t n, float* out, hipStream_t st);
+void launch_sm_zero(void* p, int64_t bytes, hipStream_t st);
+
+// ---- attention over 4-bit codes (kernels_attend.hip) ------------------------------
+struct AttendCall {
+  const IvfStore* ix;
+  const void* q; int64_t nq; int dk, v0, dtype; float scale; const int64_t* limits;
+  const int32_t* probes; int nprobe;             // null: all lists
+  const float* lse; const void* g_out; const float* g_lse;   // backward
+  void* out; float* out_lse;
+};
+struct AttendPlan {
+  int qb, nsplit, nout, lds;                     // queries a workgroup takes; parts of their rows; results; bytes of LDS
+  int64_t per, ld;                               // rows (probes) of a part; floats of a partial result
+  bool fits;
+};
+AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int nprobe, bool grad);
+void launch_attend_pad(const void* q, int64_t nq, int dk, int d, int dtype, float* out, hipStream_t st);
+// part: [nq][nsplit][ld] floats of scratch
+void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* part, hipStream_t st);
