@@ -59,7 +59,7 @@ struct ScanArgs {
   const int32_t* probes; int nprobe;      // null: all lists
   int nsplit; int64_t per;                // parts of a query's rows; rows (probes, if any) of a part
   const float* lse; const void* g_out;    // backward
-  float* part;                            // [nq][nsplit][ld]: {max, sum, out} or {sum p dp, sum p, sum p dp k, sum p k}
+  float* part;                            // [nq][nsplit][ld]: {max, sum, out}, or with w = p (dp - shift) {sum w, sum p, shift, sum w k, sum p k}
   int64_t ld;
 };
 
@@ -118,21 +118,26 @@ __device__ __forceinline__ void look_up(const float* lut, u32 word, int u, float
     acc[0] += e[0];
   }
 }
-// sum of the look-ups of sub-quantizers [m0, m1) of one row
+// Sum of the look-ups of sub-quantizers [m0, m1) of one row, in two chains: half the roundings in a row, and no addition
+// waits for the one before.  The bias, usually the largest term, comes last.
 template <int QB>
-__device__ __forceinline__ void score_row(const uint8_t* row, int cs, int m0, int m1, const float* lut, float (&acc)[QB]) {
+__device__ __forceinline__ void score_row(const uint8_t* row, int cs, int m0, int m1, const float* lut, const float* bias,
+                                          float (&out)[QB]) {
+  float acc[2][QB] = {};
   for (int w = m0 / 8; w * 8 < m1; ++w) {
     const u32 word = code_word(row, w, cs);
     const float* t = lut + (w * 8 - m0) * 16 * QB;
     if (w * 8 >= m0 && w * 8 + 8 <= m1) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) look_up<QB>(t, word, u, acc);
+      for (int u = 0; u < 8; ++u) look_up<QB>(t, word, u, acc[u & 1]);
     } else {
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (w * 8 + u >= m0 && w * 8 + u < m1) look_up<QB>(t, word, u, acc);
+        if (w * 8 + u >= m0 && w * 8 + u < m1) look_up<QB>(t, word, u, acc[u & 1]);
     }
   }
+#pragma unroll
+  for (int b = 0; b < QB; ++b) out[b] = (acc[0][b] + acc[1][b]) + bias[b];
 }
 
 template <int QB, bool GRAD>
@@ -198,14 +203,14 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       }
     }
   int64_t limit[QB];
-  float lse[QB], mx[QB], sum[QB], sum2[QB];
+  float lse[QB], mx[QB], sum[QB], sum2[QB], shift[QB];
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
     const bool in = q0 + b < A.nq;
     limit[b] = !in ? INT64_MIN : (A.limits ? A.limits[q0 + b] : INT64_MAX);
     lse[b] = GRAD && in ? A.lse[q0 + b] : 0.f;
     if (GRAD && lse[b] == neg_inf()) limit[b] = INT64_MIN;      // saw nothing
-    mx[b] = neg_inf(); sum[b] = 0.f; sum2[b] = 0.f;
+    mx[b] = neg_inf(); sum[b] = 0.f; sum2[b] = 0.f; shift[b] = 0.f;
   }
   const int rs = lane / (L.mh < 64 ? L.mh : 64), hm = lane % (L.mh < 64 ? L.mh : 64);
   const int rstep = L.mh < 64 ? 64 / L.mh : 1;
@@ -281,9 +286,9 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     }
     __syncthreads();
     // scores
-    float top[QB];
+    float top[QB], rp[QB], rw[QB];
 #pragma unroll
-    for (int b = 0; b < QB; ++b) top[b] = neg_inf();
+    for (int b = 0; b < QB; ++b) { top[b] = neg_inf(); rp[b] = 0.f; rw[b] = 0.f; }
     int tile = 0;
     for (int s = 0; s < nseg; ++s) {
       const Segment sg = segs[s];
@@ -294,10 +299,8 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
           const int64_t pos = sg.pos + i;
           const int64_t id = A.limits ? A.ids[pos] : 0;
           float acc[QB], acc2[QB];
-#pragma unroll
-          for (int b = 0; b < QB; ++b) { acc[b] = lds[L.bias + s * QB + b]; acc2[b] = GRAD ? lds[L.bias2 + s * QB + b] : 0.f; }
-          score_row<QB>(A.codes + pos * cs, cs, 0, mk, lds + L.lut, acc);
-          if (GRAD) score_row<QB>(A.codes + pos * cs, cs, mv0, M, lds + L.lut2, acc2);
+          score_row<QB>(A.codes + pos * cs, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
+          if (GRAD) score_row<QB>(A.codes + pos * cs, cs, mv0, M, lds + L.lut2, lds + L.bias2 + s * QB, acc2);
 #pragma unroll
           for (int b = 0; b < QB; ++b) {
             const bool sees = id < limit[b];
@@ -305,9 +308,9 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
               const float p = sees ? exp_neg(acc[b] - lse[b]) : 0.f;
               const float w = sees ? p * acc2[b] : 0.f;
               lds[L.score + (sg.first + i) * QB + b] = p;
-              lds[L.score2 + (sg.first + i) * QB + b] = w;
-              sum[b] += p;
-              sum2[b] += w;
+              lds[L.score2 + (sg.first + i) * QB + b] = acc2[b];
+              rp[b] += p;
+              rw[b] += w;
             } else {
               const float v = sees ? acc[b] : neg_inf();
               lds[L.score + (sg.first + i) * QB + b] = v;
@@ -345,6 +348,29 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
         const float p = v == neg_inf() ? 0.f : exp_neg(v - mx[b]);
         lds[L.score + i] = p;
         if (QB == 1) sum[0] += p; else if (b == 0) sum[0] += p; else sum[QB - 1] += p;
+      }
+    }
+    if (GRAD) {
+      // The sums of p dp k and (sum p dp) p k nearly cancel; taken relative to the mean of dp over the part's first round
+      // with any weight they do not.
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+        rp[b] = wave_sum(rp[b]);
+        rw[b] = wave_sum(rw[b]);
+        if (lane == 0) { lds[L.red + wave * 2 * QB + b] = rp[b]; lds[L.red + wave * 2 * QB + QB + b] = rw[b]; }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+        float p = 0.f, w = 0.f;
+        for (int v = 0; v < kWaves; ++v) { p += lds[L.red + v * 2 * QB + b]; w += lds[L.red + v * 2 * QB + QB + b]; }
+        if (!(mx[b] > neg_inf()) && p > 0.f) { shift[b] = w / p; mx[b] = 0.f; }      // (mx: whether the shift is set)
+      }
+      for (int i = threadIdx.x; i < rows * QB; i += 256) {
+        const int b = QB == 1 ? 0 : i % QB;
+        const float p = lds[L.score + i], w = p == 0.f ? 0.f : p * (lds[L.score2 + i] - (b == 0 ? shift[0] : shift[QB - 1]));
+        lds[L.score2 + i] = w;
+        if (b == 0) { sum[0] += p; sum2[0] += w; } else { sum[QB - 1] += p; sum2[QB - 1] += w; }
       }
     }
     __syncthreads();
@@ -459,6 +485,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       for (int w = 0; w < kWaves; ++w) { s += lds[L.red + w * 2 * QB + b]; s2 += lds[L.red + w * 2 * QB + QB + b]; }
       out[0] = GRAD ? s2 : mx[b];
       out[1] = s;
+      if (GRAD) out[2] = shift[b];
     }
     for (int i = threadIdx.x; i < SETS * nout; i += 256) {
       const int set = i / nout, t = i - set * nout, m = t / dsub, u = t - m * dsub;
@@ -467,7 +494,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       float v = lds[L.cacc + (set * QB + b) * nout + t];
 #pragma unroll
       for (int c = 0; c < 16; ++c) v = __builtin_fmaf(h[c * 64], cb[c * dsub], v);
-      out[2 + i] = v;
+      out[(GRAD ? 3 : 2) + i] = v;
     }
   }
 }
@@ -493,13 +520,21 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
     }
     if (out_lse && threadIdx.x == 0) out_lse[qi] = l == 0.f ? neg_inf() : m + logf(l);
   } else {
-    float dmean = 0.f;
-    for (int s = 0; s < nsplit; ++s) dmean += p[s * ld];
-    const float shift = dmean - (g_lse ? g_lse[qi] : 0.f);
+    // sum p (dp - mean + g_lse) k, every part relative to its own shift of dp
+    // (mean of dp under weights that sum to 1 up to the roundings of scores and lse: divided by their own sum, a common
+    // factor of all weights leaves it as it is)
+    float mean = 0.f, total = 0.f;
+    for (int s = 0; s < nsplit; ++s) {
+      mean += __builtin_fmaf(p[s * ld + 2], p[s * ld + 1], p[s * ld]);
+      total += p[s * ld + 1];
+    }
+    if (total != 0.f) mean /= total;
+    const float gl = g_lse ? g_lse[qi] : 0.f;
     for (int t = threadIdx.x; t < nout; t += 256) {
-      float a = 0.f, b = 0.f;
-      for (int s = 0; s < nsplit; ++s) { a += p[s * ld + 2 + t]; b += p[s * ld + 2 + nout + t]; }
-      store_as(out, qi * nout + t, dtype, scale * __builtin_fmaf(-shift, b, a));
+      float a = 0.f;
+      for (int s = 0; s < nsplit; ++s)
+        a += __builtin_fmaf(p[s * ld + 2] - mean + gl, p[s * ld + 3 + nout + t], p[s * ld + 3 + t]);
+      store_as(out, qi * nout + t, dtype, scale * a);
     }
   }
 }
@@ -526,7 +561,7 @@ int scan_queries(const IvfpqDims& g, int dk, int v0, int64_t nq, bool probed, bo
 AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int nprobe, bool grad) {
   AttendPlan p;
   p.nout = grad ? dk : g.d - v0;
-  p.ld = 2 + (grad ? 2 : 1) * (int64_t)p.nout;
+  p.ld = grad ? 3 + 2 * (int64_t)p.nout : 2 + p.nout;
   p.qb = scan_queries(g, dk, v0, nq, nprobe > 0, grad);
   p.lds = scan_lds(g, dk, v0, p.qb, grad).total * 4;
   p.fits = p.lds <= kMaxLds;
