@@ -65,6 +65,14 @@ struct ScanArgs {
 
 struct Segment { int64_t pos; int32_t list, first, len, pad; };   // rows [first, first + len) of a round
 
+// The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
+// not wait for them, and the compiler does not always count the wait states across the end of a loop.  20 cover any product.
+__device__ __forceinline__ void settle_products() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // What a workgroup of QB queries keeps in LDS, in floats.
 struct ScanLds {
   int lut, lut2, q, g, score, score2, hist, cacc, codes, bias, bias2, red, seg, total;
@@ -499,44 +507,629 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   }
 }
 
-// One workgroup per query: parts joined under their common maximum (forward) or added (backward).
+
+// ---- many queries over whole lists: decoded tiles on the matrix cores ------------------------------
+// Queries of one call share their rows when all lists are read, and a row decoded once serves 16 or 64 of them: the
+// operands of v_mfma_f32_16x16x32_f16 are put together in registers from codeword tables in LDS, nothing is decoded to
+// memory.  A tile is 64 rows by 16 NQ queries:
+//   scores  S^T = K q^T: a wavefront takes 16 rows (operand A: lane = row lane & 15, 8 components a step; a lane of group
+//           g = lane >> 4 goes through the codes [g mq, (g + 1) mq) of its row, so its code bytes are consecutive; a
+//           codeword is looked up in pieces of W components, {W heads, W tails}, padded to whole pieces),
+//   weights p = e^(s - m) 2^14 in fp16 (fp32 queries: head and tail) through LDS, to lie along rows,
+//   product O^T = V^T p^T: a wavefront takes 16 components of every 64 (operand A: lane = component, 8 rows a step,
+//           looked up one by one in a table [component][16]).
+// The centroid of a list adds a constant to its scores and sum(p) centroid to the product, both once per list and part.
+// The tables are relative to a power of two each and keep head and tail (22 bits), so scores are good to fp32; weights
+// keep 11 bits for 16-bit queries, whose results have no more, and 22 for fp32.
+// The gradient's tile computes p from lse and the product of g with the values, w = p <g, t> and adds w k and p k; both
+// relative to the centroid part of <g, v> of the present list, which is exchanged when the list changes.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTileRows = 64;
+constexpr int kTableBits = 14;                 // weights are held times 2^14
+
+struct CodeSet {                               // sub-quantizers [m0, m0 + n) as rows of an operand
+  int m0, n, mq, ppc, steps, stride, entry;    // codes of a lane group, pieces of a codeword, steps; bytes of a staged row, of a piece
+};
+__host__ __device__ inline CodeSet code_set(int m0, int n, int dsub, int w) {
+  CodeSet c;
+  const int per = 8 / w;
+  c.m0 = m0; c.n = n;
+  c.mq = ((n + 3) / 4 + per - 1) / per * per;
+  c.ppc = (dsub + w - 1) / w;
+  c.steps = c.ppc * c.mq / per;
+  c.stride = 4 * c.mq + 4;
+  c.entry = 4 * w;
+  return c;
+}
+struct TileLds {                               // bytes
+  int ktab, gtab, vtab, qf, gf, krow, grow, vcol, p, ids, red, stat, cent, total;
+  int p_stride, p_set;
+};
+__host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, int w, int nq, int planes, bool grad) {
+  TileLds o{};
+  int at = 0;
+  auto take = [&](int n) { const int b = at; at += (n + 15) / 16 * 16; return b; };
+  const int dv = g.d - v0, mk = dk / g.dsub, mv = dv / g.dsub;
+  const CodeSet k = code_set(0, mk, g.dsub, w), v = code_set(g.M - mv, mv, g.dsub, w);
+  const int nout = grad ? dk : dv, mo = grad ? mk : mv;
+  o.ktab = take(k.ppc * 4 * k.mq * 16 * k.entry);
+  o.gtab = take(grad ? v.ppc * 4 * v.mq * 16 * v.entry : 0);
+  o.vtab = take((nout + 15) / 16 * 16 * 64);
+  o.qf = take(planes * nq * k.steps * 1024);
+  o.gf = take(grad ? planes * nq * v.steps * 1024 : 0);
+  o.krow = take(kTileRows * k.stride);
+  o.grow = take(grad ? kTileRows * v.stride : 0);
+  o.vcol = take(mo * 72);
+  o.p_stride = kTileRows * 2 + 16;
+  o.p_set = planes * nq * 16 * o.p_stride;
+  o.p = take((grad ? 2 : 1) * o.p_set);
+  o.ids = take(kTileRows * 8);
+  o.red = take(4 * 2 * nq * 16 * 4);
+  o.stat = take(nq * 16 * 6 * 4);
+  o.cent = take((dk + dv) * 4);
+  o.total = at;
+  return o;
+}
+
+// The power of two that brings `mx` into [1, 2), as factor up and its inverse
+__device__ __forceinline__ void unit_scale(float mx, float* up, float* down) {
+  int e = mx > 0.f && mx < __builtin_inff() ? 1 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
+  e = e < -120 ? -120 : (e > 120 ? 120 : e);
+  *up = __builtin_ldexpf(1.f, e);
+  *down = __builtin_ldexpf(1.f, -e);
+}
+__device__ __forceinline__ u32 pack_parts(float v) {     // {head, tail}
+  const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
+  return (u32)__builtin_bit_cast(unsigned short, hi) | (u32)__builtin_bit_cast(unsigned short, lo) << 16;
+}
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Table of a code set: piece (j, code) of codeword c at ((j 4 mq + code) 16 + c) entry bytes, {W heads, W tails}.
+template <int W>
+__device__ __forceinline__ void build_rows_table(char* tab, const CodeSet& c, const float* codebooks, int dsub, float up) {
+  const int n = c.ppc * 4 * c.mq * 16;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int w = i & 15, jc = i >> 4, code = jc % (4 * c.mq), j = jc / (4 * c.mq);
+    _Float16* e = reinterpret_cast<_Float16*>(tab + i * c.entry);
+#pragma unroll
+    for (int t = 0; t < W; ++t) {
+      const int u = j * W + t;
+      const float v = code < c.n && u < dsub ? codebooks[((int64_t)(c.m0 + code) * 16 + w) * dsub + u] * up : 0.f;
+      const _Float16 hi = (_Float16)v;
+      e[t] = hi;
+      e[W + t] = (_Float16)(v - (float)hi);
+    }
+  }
+}
+// Operand B of a code set: the vectors' components in the order of the lanes' steps, [plane][block of 16][step][64 lanes].
+template <int W, int PL>
+__device__ __forceinline__ void build_query_fragments(char* out, const CodeSet& c, int nqb, const void* src, int64_t ld,
+                                                      int dtype, int64_t q0, int64_t nq, int dsub, const float* up) {
+  constexpr int PER = 8 / W;
+  const int n = nqb * c.steps * 64;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int l = i & 63, step = (i >> 6) % c.steps, qb = (i >> 6) / c.steps;
+    const int per_j = c.mq / PER, j = step / per_j, s = step - j * per_j, g = l >> 4;
+    const int ql = qb * 16 + (l & 15);
+    const int64_t qi = q0 + ql;
+    f16x8 hi, lo;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const int code = g * c.mq + s * PER + t / W, u = j * W + t % W;
+      float v = 0.f;
+      if (qi < nq && code < c.n && u < dsub) v = load_as_f32(src, qi * ld + code * dsub + u, dtype) * up[ql];
+      hi[t] = (_Float16)v;
+      lo[t] = (_Float16)(v - (float)hi[t]);
+    }
+    reinterpret_cast<f16x8*>(out)[i] = hi;
+    if (PL == 2) reinterpret_cast<f16x8*>(out)[n + i] = lo;
+  }
+}
+
+// acc[qb] += rows (16 of this wavefront) x queries over a code set; acc's lane: query lane & 15, rows 4 (lane >> 4) + r
+template <int W, int NQ, int PL>
+__device__ __forceinline__ void rows_product(const char* tab, const CodeSet& c, const char* rows, const char* frag, f32x4 (&acc)[NQ]) {
+  constexpr int PER = 8 / W;
+  const int lane = lane_id(), g = lane >> 4;
+  const char* mine = rows + ((threadIdx.x >> 6) * 16 + (lane & 15)) * c.stride + g * c.mq;
+  const u32x4* b = reinterpret_cast<const u32x4*>(frag) + lane;
+  const int n = NQ * c.steps * 64;
+  for (int j = 0; j < c.ppc; ++j) {
+    const char* t = tab + (j * 4 + g) * c.mq * 16 * c.entry;
+    for (int s = 0; s < c.mq / PER; ++s) {
+      u32 bytes;
+      if (W == 4) bytes = *reinterpret_cast<const unsigned short*>(mine + s * 2);
+      else bytes = *reinterpret_cast<const u32*>(mine + s * 4);
+      u32x4 hi, lo;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const char* e = t + (s * PER + i) * 16 * c.entry + ((bytes >> (8 * i)) & 15u) * c.entry;
+        if (W == 4) {
+          const u32x4 v = *reinterpret_cast<const u32x4*>(e);
+          hi[2 * i] = v[0]; hi[2 * i + 1] = v[1]; lo[2 * i] = v[2]; lo[2 * i + 1] = v[3];
+        } else {
+          const u32x2 v = *reinterpret_cast<const u32x2*>(e);
+          hi[i] = v[0]; lo[i] = v[1];
+        }
+      }
+      const int step = j * (c.mq / PER) + s;
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        const u32x4 q = b[(qb * c.steps + step) * 64];
+        acc[qb] = mma(hi, q, acc[qb]);
+        acc[qb] = mma(lo, q, acc[qb]);
+        if (PL == 2) acc[qb] = mma(hi, b[n + (qb * c.steps + step) * 64], acc[qb]);
+      }
+    }
+  }
+  settle_products();
+}
+
+constexpr int SETS_OF(bool grad) { return grad ? 2 : 1; }
+template <int W, int NQ, int NB, int PL, bool GRAD>
+__global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void attend_tiles_kernel(ScanArgs A) {
+  extern __shared__ __align__(16) char ldsb[];
+  const TileLds L = tile_lds(A.g, A.dk, A.v0, W, NQ, PL, GRAD);
+  constexpr int QT = NQ * 16, SETS = GRAD ? 2 : 1;
+  const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+  const int d = A.g.d, dsub = A.g.dsub, M = A.g.M, cs = A.g.code_size, dv = d - A.v0;
+  const int mk = A.dk / dsub, mv = dv / dsub, mv0 = M - mv;
+  const CodeSet K = code_set(0, mk, dsub, W), V = code_set(mv0, mv, dsub, W);
+  const int nout = GRAD ? A.dk : dv, om0 = GRAD ? 0 : mv0, mo = GRAD ? mk : mv;
+  const int split = blockIdx.x % A.nsplit;
+  const int64_t q0 = (int64_t)(blockIdx.x / A.nsplit) * QT;
+  const int64_t r0 = split * A.per, r1 = r0 + A.per < A.ntotal ? r0 + A.per : A.ntotal;
+  float* red = reinterpret_cast<float*>(ldsb + L.red);
+  float* stat = reinterpret_cast<float*>(ldsb + L.stat);     // per query: up, down of q; up, down of g; bound of w; bias
+  int64_t* ids = reinterpret_cast<int64_t*>(ldsb + L.ids);
+  float* cent = reinterpret_cast<float*>(ldsb + L.cent);     // centroid of the list: [dk] keys, [dv] values
+
+  // scales: of the key and value codewords, and of every query
+  float km = 0.f, vm = 0.f;
+  for (int i = threadIdx.x; i < mk * 16 * dsub; i += 256) km = fmaxf(km, fabsf(A.codebooks[i]));
+  for (int i = threadIdx.x; i < mv * 16 * dsub; i += 256) vm = fmaxf(vm, fabsf(A.codebooks[(int64_t)mv0 * 16 * dsub + i]));
+  km = wave_max(km);
+  vm = wave_max(vm);
+  if (lane == 0) { red[wave] = km; red[4 + wave] = vm; }
+  __syncthreads();
+  km = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  vm = fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
+  float k_up, k_down, v_up, v_down;
+  unit_scale(km, &k_up, &k_down);
+  unit_scale(vm, &v_up, &v_down);
+  for (int ql = wave; ql < QT; ql += 4) {
+    const int64_t qi = q0 + ql;
+    float mx = 0.f, gx = 0.f, g1 = 0.f;
+    if (qi < A.nq) {
+      for (int t = lane; t < A.dk; t += 64) mx = fmaxf(mx, fabsf(load_as_f32(A.q, qi * A.dk + t, A.dtype)));
+      if (GRAD)
+        for (int t = lane; t < dv; t += 64) {
+          const float v = fabsf(load_as_f32(A.g_out, qi * dv + t, A.dtype));
+          gx = fmaxf(gx, v);
+          g1 += v;
+        }
+    }
+    mx = wave_max(mx);
+    float up, down;
+    unit_scale(mx, &up, &down);
+    if (lane == 0) { stat[ql] = up; stat[QT + ql] = down; }
+    if (GRAD) {
+      gx = wave_max(gx);
+      g1 = wave_sum(g1);
+      float gup, gdown, bup, bdown;
+      unit_scale(gx, &gup, &gdown);
+      unit_scale(g1 * vm, &bup, &bdown);                     // |<g, t>| <= |g|_1 max |t| < 2 bdown
+      if (lane == 0) { stat[2 * QT + ql] = gup; stat[3 * QT + ql] = gdown; stat[4 * QT + ql] = bdown; }
+    }
+  }
+  __syncthreads();
+  build_rows_table<W>(ldsb + L.ktab, K, A.codebooks, dsub, k_up);
+  if (GRAD) build_rows_table<W>(ldsb + L.gtab, V, A.codebooks, dsub, v_up);
+  const float o_up = GRAD ? k_up : v_up, o_down = GRAD ? k_down : v_down;
+  for (int i = threadIdx.x; i < (nout + 15) / 16 * 256; i += 256) {
+    const int t = i >> 4, c = i & 15, m = t / dsub;
+    reinterpret_cast<u32*>(ldsb + L.vtab)[i] = t < nout ? pack_parts(A.codebooks[((int64_t)(om0 + m) * 16 + c) * dsub + t - m * dsub] * o_up) : 0u;
+  }
+  build_query_fragments<W, PL>(ldsb + L.qf, K, NQ, A.q, A.dk, A.dtype, q0, A.nq, dsub, stat);
+  if (GRAD) build_query_fragments<W, PL>(ldsb + L.gf, V, NQ, A.g_out, dv, A.dtype, q0, A.nq, dsub, stat + 2 * QT);
+
+  int64_t limit[NQ], seen_to = INT64_MIN;
+  float fs[NQ], fg[NQ], fw[NQ], lse[NQ], bias[NQ], mx[NQ], lp[NQ], lw[NQ], sum[NQ], sum2[NQ];
+  f32x4 o[SETS][NB][NQ] = {};
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const int64_t qi = q0 + qb * 16 + col;
+    const bool in = qi < A.nq;
+    limit[qb] = !in ? INT64_MIN : (A.limits ? A.limits[qi] : INT64_MAX);
+    lse[qb] = GRAD && in ? A.lse[qi] : 0.f;
+    if (GRAD && lse[qb] == neg_inf()) limit[qb] = INT64_MIN;
+    fs[qb] = A.scale * (k_down * stat[QT + qb * 16 + col]);
+    fg[qb] = GRAD ? v_down * stat[3 * QT + qb * 16 + col] : 0.f;
+    fw[qb] = GRAD ? 1.f / stat[4 * QT + qb * 16 + col] : 0.f;
+    mx[qb] = neg_inf(); lp[qb] = 0.f; lw[qb] = 0.f; sum[qb] = 0.f; sum2[qb] = 0.f; bias[qb] = 0.f;
+    seen_to = limit[qb] > seen_to ? limit[qb] : seen_to;
+  }
+#pragma unroll
+  for (int w = 1; w < 16; w <<= 1) { const int64_t t = __shfl_xor(seen_to, w); seen_to = t > seen_to ? t : seen_to; }
+  int vdim[NB];                                              // this lane's components' columns of staged codes
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int t = (nb * 4 + wave) * 16 + col;
+    vdim[nb] = (t < nout ? t : nout - 1) / dsub * 72;
+  }
+
+  // sums over the list that ends: centroid parts of the results, and (gradient) the exchange of <g, centroid>
+  float gbias[NQ], shift[NQ];
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) { gbias[qb] = 0.f; shift[qb] = 0.f; }
+  int list = -1;
+  auto close_list = [&]() {
+    if (list < 0) return;
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      float p = lp[qb], w = lw[qb];
+      p += __shfl_xor(p, 16); p += __shfl_xor(p, 32);
+      if (GRAD) { w += __shfl_xor(w, 16); w += __shfl_xor(w, 32); }
+      if (g == 0) { red[(wave * 2) * QT + qb * 16 + col] = p; if (GRAD) red[(wave * 2 + 1) * QT + qb * 16 + col] = w; }
+      lp[qb] = 0.f; lw[qb] = 0.f;
+    }
+    __syncthreads();
+    const float* c = GRAD ? cent : cent + A.dk;
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      float p = 0.f, w = 0.f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) { p += red[(v * 2) * QT + qb * 16 + col]; if (GRAD) w += red[(v * 2 + 1) * QT + qb * 16 + col]; }
+      sum[qb] += p;
+      sum2[qb] += w;
+      // o is held times 2^14 / o_down (w also over its bound)
+      const float ps = p * o_up * (float)(1 << kTableBits), ws = GRAD ? w * fw[qb] * o_up * (float)(1 << kTableBits) : 0.f;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int t = (nb * 4 + wave) * 16 + 4 * g + r;
+          const float cv = t < nout ? c[t] : 0.f;
+          o[SETS - 1][nb][qb][r] = __builtin_fmaf(cv, ps, o[SETS - 1][nb][qb][r]);
+          if (GRAD) o[0][nb][qb][r] = __builtin_fmaf(cv, ws, o[0][nb][qb][r]);
+        }
+    }
+    __syncthreads();
+  };
+  auto open_list = [&](int l) {
+    list = l;
+    const float* c = A.centroids + (int64_t)l * d;
+    for (int t = threadIdx.x; t < A.dk; t += 256) cent[t] = c[t];
+    for (int t = threadIdx.x; t < dv; t += 256) cent[A.dk + t] = c[A.v0 + t];
+    __syncthreads();
+    for (int ql = wave; ql < QT; ql += 4) {                  // <q, c>, <g, c> in fp32
+      const int64_t qi = q0 + ql;
+      float s = 0.f, s2 = 0.f;
+      if (qi < A.nq) {
+        for (int t = lane; t < A.dk; t += 64) s = __builtin_fmaf(load_as_f32(A.q, qi * A.dk + t, A.dtype), cent[t], s);
+        if (GRAD)
+          for (int t = lane; t < dv; t += 64) s2 = __builtin_fmaf(load_as_f32(A.g_out, qi * dv + t, A.dtype), cent[A.dk + t], s2);
+      }
+      s = wave_sum(s);
+      if (GRAD) s2 = wave_sum(s2);
+      if (lane == 0) { red[ql] = s * A.scale; red[QT + ql] = s2; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      bias[qb] = red[qb * 16 + col];
+      if (GRAD) {                                            // sums relative to the new list's <g, c>
+        const float now = red[QT + qb * 16 + col], by = gbias[qb] - now;
+        sum2[qb] = __builtin_fmaf(by, sum[qb], sum2[qb]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[0][nb][qb][r] = __builtin_fmaf(by * fw[qb], o[1][nb][qb][r], o[0][nb][qb][r]);
+        gbias[qb] = now;
+      }
+    }
+    __syncthreads();
+  };
+
+  // a tile's codes and ids, one tile ahead in registers: thread = row lane, words wave, wave + 4, ..
+  constexpr int kWords = 4;
+  const int words = (cs + 3) / 4;
+  u32 ahead[kWords];
+  int64_t ahead_id = 0;
+  auto fetch = [&](int64_t pos, int n) {
+    const bool in = lane < n;
+    const uint8_t* row = A.codes + (pos + (in ? lane : 0)) * cs;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int w = wave + 4 * i;
+      ahead[i] = in && w < words ? code_word(row, w, cs) : 0u;
+    }
+    ahead_id = in && A.limits ? A.ids[pos + lane] : 0;
+  };
+
+  int64_t pos = r0;
+  int cur = -1;
+  int64_t cur_end = r0;
+  auto advance = [&]() {                                      // list and end of the run that pos lies in
+    if (pos < r1 && pos >= cur_end) {
+      cur = cur < 0 ? list_of_position(A.list_off, A.g.nlist, pos) : cur + 1;
+      while (A.list_off[cur + 1] <= pos) ++cur;
+      cur_end = A.list_off[cur + 1] < r1 ? A.list_off[cur + 1] : r1;
+    }
+  };
+  advance();
+  int n = pos < r1 ? (int)(cur_end - pos < kTileRows ? cur_end - pos : kTileRows) : 0;
+  if (n > 0) fetch(pos, n);
+  while (n > 0) {
+    const int here = n, here_list = cur;
+    const int64_t my_id = ahead_id;
+    u32 word[kWords];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) word[i] = ahead[i];
+    pos += n;
+    advance();
+    n = pos < r1 ? (int)(cur_end - pos < kTileRows ? cur_end - pos : kTileRows) : 0;
+    const bool any = __ballot(lane < here && my_id < seen_to) != 0;   // (the same rows in every wavefront)
+    if (n > 0) fetch(pos, n);
+    if (!any) continue;
+    if (here_list != list) { close_list(); open_list(here_list); }
+    else __syncthreads();                                     // the tile before has been read
+    // codes as bytes: along rows for the scores, along components for the product
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const int w = wave + 4 * i;
+      if (w < words) {
+      const u32 even = word[i] & 0x0F0F0F0Fu, odd = (word[i] >> 4) & 0x0F0F0F0Fu;
+      const u32 b0 = __builtin_amdgcn_perm(odd, even, 0x05010400u), b1 = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+      const int m = w * 8;
+      auto row_bytes = [&](char* rows, const CodeSet& c) {
+        const int at = m - c.m0;
+        char* out = rows + lane * c.stride;
+        if (at >= 0 && at + 8 <= 4 * c.mq && (at & 3) == 0) {
+          *reinterpret_cast<u32*>(out + at) = b0;
+          *reinterpret_cast<u32*>(out + at + 4) = b1;
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (at + u >= 0 && at + u < 4 * c.mq) out[at + u] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+        }
+      };
+      row_bytes(ldsb + L.krow, K);
+      if (GRAD) row_bytes(ldsb + L.grow, V);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (m + u >= om0 && m + u < om0 + mo) (ldsb + L.vcol)[(m + u - om0) * 72 + lane] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+      }
+    }
+    if (wave == 0) ids[lane] = my_id;
+    __syncthreads();
+    f32x4 s[NQ] = {}, t[NQ] = {};
+    rows_product<W, NQ, PL>(ldsb + L.ktab, K, ldsb + L.krow, ldsb + L.qf, s);
+    if (GRAD) rows_product<W, NQ, PL>(ldsb + L.gtab, V, ldsb + L.grow, ldsb + L.gf, t);
+    const int row = wave * 16 + 4 * g;
+    bool row_in[4];
+    int64_t row_id[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) { row_in[r] = row + r < here; row_id[r] = ids[row + r]; }
+    if (!GRAD) {
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        float m = neg_inf();
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float v = __builtin_fmaf(s[qb][r], fs[qb], bias[qb]);
+          s[qb][r] = row_in[r] && row_id[r] < limit[qb] ? v : neg_inf();
+          m = fmaxf(m, s[qb][r]);
+        }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        if (g == 0) red[wave * QT + qb * 16 + col] = m;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        float m = mx[qb];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, red[v * QT + qb * 16 + col]);
+        if (m > mx[qb]) {
+          const float f = mx[qb] == neg_inf() ? 1.f : exp_neg(mx[qb] - m);      // (nothing yet: zeros to scale)
+          lp[qb] *= f;
+          sum[qb] *= f;
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) o[0][nb][qb] *= f;
+          mx[qb] = m;
+        }
+      }
+    }
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      const float base = GRAD ? lse[qb] : (mx[qb] > neg_inf() ? mx[qb] : 0.f);
+      u32 ph[2], pl[2], wh[2], wl[2];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float p, w = 0.f;
+        if (GRAD) {
+          const bool sees = row_in[r] && row_id[r] < limit[qb];
+          p = sees ? exp_neg(__builtin_fmaf(s[qb][r], fs[qb], bias[qb]) - base) : 0.f;
+          w = sees ? p * (t[qb][r] * fg[qb]) : 0.f;
+          lw[qb] += w;
+        } else {
+          p = exp_neg(s[qb][r] - base);
+        }
+        lp[qb] += p;
+        const u32 pp = pack_parts(p * (float)(1 << kTableBits)), pw = GRAD ? pack_parts(w * fw[qb] * (float)(1 << kTableBits)) : 0u;
+        if (r & 1) {
+          ph[r >> 1] |= pp << 16; pl[r >> 1] |= pp & 0xFFFF0000u;
+          wh[r >> 1] |= pw << 16; wl[r >> 1] |= pw & 0xFFFF0000u;
+        } else {
+          ph[r >> 1] = pp & 0xFFFFu; pl[r >> 1] = pp >> 16;
+          wh[r >> 1] = pw & 0xFFFFu; wl[r >> 1] = pw >> 16;
+        }
+      }
+      char* out = ldsb + L.p + (SETS - 1) * L.p_set + (qb * 16 + col) * L.p_stride + row * 2;
+      *reinterpret_cast<u32x2*>(out) = u32x2{ph[0], ph[1]};
+      if (PL == 2) *reinterpret_cast<u32x2*>(out + QT * L.p_stride) = u32x2{pl[0], pl[1]};
+      if (GRAD) {
+        out -= L.p_set;
+        *reinterpret_cast<u32x2*>(out) = u32x2{wh[0], wh[1]};
+        if (PL == 2) *reinterpret_cast<u32x2*>(out + QT * L.p_stride) = u32x2{wl[0], wl[1]};
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 b[SETS][PL][NQ];
+#pragma unroll
+      for (int st = 0; st < SETS; ++st)
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+          for (int qb = 0; qb < NQ; ++qb)
+            b[st][pl][qb] = *reinterpret_cast<const u32x4*>(ldsb + L.p + st * L.p_set + (pl * QT + qb * 16 + col) * L.p_stride + ks * 64 + g * 16);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const int t0 = (nb * 4 + wave) * 16;
+        if (t0 < nout) {
+        const u32x2 c8 = *reinterpret_cast<const u32x2*>(ldsb + L.vcol + vdim[nb] + ks * 32 + g * 8);
+        const char* tab = ldsb + L.vtab + (t0 + col) * 64;
+        u32 e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const u32 c = (c8[i >> 2] >> (8 * (i & 3))) & 15u;
+          e[i] = *reinterpret_cast<const u32*>(tab + c * 4);
+        }
+        u32x4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          hi[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x05040100u);
+          lo[i] = __builtin_amdgcn_perm(e[2 * i + 1], e[2 * i], 0x07060302u);
+        }
+#pragma unroll
+        for (int st = 0; st < SETS; ++st)
+#pragma unroll
+          for (int qb = 0; qb < NQ; ++qb) {
+            o[st][nb][qb] = mma(hi, b[st][0][qb], o[st][nb][qb]);
+            o[st][nb][qb] = mma(lo, b[st][0][qb], o[st][nb][qb]);
+            if (PL == 2) o[st][nb][qb] = mma(hi, b[st][PL - 1][qb], o[st][nb][qb]);
+          }
+        }
+      }
+    }
+    settle_products();
+  }
+  close_list();
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const int64_t qi = q0 + qb * 16 + col;
+    if (qi >= A.nq) continue;
+    float* out = A.part + (qi * A.nsplit + split) * A.ld;
+    const float f = o_down * (1.f / (float)(1 << kTableBits));
+    if (wave == 0 && g == 0) {
+      out[0] = GRAD ? sum2[qb] : mx[qb];
+      out[1] = sum[qb];
+      if (GRAD) out[2] = gbias[qb];
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = (nb * 4 + wave) * 16 + 4 * g + r;
+        if (t >= nout) continue;
+        if (GRAD) {
+          out[3 + t] = o[0][nb][qb][r] * (f * stat[4 * QT + qb * 16 + col]);
+          out[3 + nout + t] = o[SETS - 1][nb][qb][r] * f;
+        } else {
+          out[2 + t] = o[0][nb][qb][r] * f;
+        }
+      }
+  }
+}
+
+// Parts joined under their common maximum (forward) or added (backward): a workgroup takes 64 results of a query.  The
+// parts' factors come first, a part a thread; then four wavefronts go through the parts, eight loads in flight each.
+constexpr int kMaxParts = 2048;
 template <bool GRAD>
 __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restrict__ part, int nsplit, int64_t ld, int nout,
                                                           const float* __restrict__ g_lse, float scale, int dtype,
                                                           void* __restrict__ out, float* __restrict__ out_lse) {
+  __shared__ float factor[kMaxParts];
+  __shared__ float red[8];
+  __shared__ float sums[4][64];
   const int64_t qi = blockIdx.x;
+  const int lane = lane_id(), wave = threadIdx.x >> 6, t = blockIdx.y * 64 + lane;
   const float* p = part + qi * nsplit * ld;
+  float inv = 1.f;
   if (!GRAD) {
     float m = neg_inf();
-    for (int s = 0; s < nsplit; ++s) m = fmaxf(m, p[s * ld]);
+    for (int s = threadIdx.x; s < nsplit; s += 256) m = fmaxf(m, p[s * ld]);
+    m = wave_max(m);
+    if (lane == 0) red[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     float l = 0.f;
-    for (int s = 0; s < nsplit; ++s) l += p[s * ld] == neg_inf() ? p[s * ld + 1] : p[s * ld + 1] * exp_neg(p[s * ld] - m);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    for (int t = threadIdx.x; t < nout; t += 256) {
-      float v = 0.f;
-      for (int s = 0; s < nsplit; ++s)
-        if (p[s * ld] != neg_inf()) v = __builtin_fmaf(p[s * ld + 2 + t], exp_neg(p[s * ld] - m), v);
-      store_as(out, qi * nout + t, dtype, v * inv);
+    for (int s = threadIdx.x; s < nsplit; s += 256) {
+      const float f = p[s * ld] == neg_inf() ? 0.f : exp_neg(p[s * ld] - m);
+      factor[s] = f;
+      l += f == 0.f && p[s * ld] == neg_inf() ? p[s * ld + 1] : p[s * ld + 1] * f;    // (0, or a NaN, of a part without maximum)
     }
-    if (out_lse && threadIdx.x == 0) out_lse[qi] = l == 0.f ? neg_inf() : m + logf(l);
+    l = wave_sum(l);
+    if (lane == 0) red[4 + wave] = l;
+    __syncthreads();
+    l = red[4] + red[5] + red[6] + red[7];
+    inv = l == 0.f ? 0.f : 1.f / l;
+    if (out_lse && blockIdx.y == 0 && threadIdx.x == 0) out_lse[qi] = l == 0.f ? neg_inf() : m + logf(l);
   } else {
     // sum p (dp - mean + g_lse) k, every part relative to its own shift of dp
     // (mean of dp under weights that sum to 1 up to the roundings of scores and lse: divided by their own sum, a common
     // factor of all weights leaves it as it is)
     float mean = 0.f, total = 0.f;
-    for (int s = 0; s < nsplit; ++s) {
+    for (int s = threadIdx.x; s < nsplit; s += 256) {
       mean += __builtin_fmaf(p[s * ld + 2], p[s * ld + 1], p[s * ld]);
       total += p[s * ld + 1];
     }
+    mean = wave_sum(mean);
+    total = wave_sum(total);
+    if (lane == 0) { red[wave] = mean; red[4 + wave] = total; }
+    __syncthreads();
+    mean = red[0] + red[1] + red[2] + red[3];
+    total = red[4] + red[5] + red[6] + red[7];
     if (total != 0.f) mean /= total;
     const float gl = g_lse ? g_lse[qi] : 0.f;
-    for (int t = threadIdx.x; t < nout; t += 256) {
-      float a = 0.f;
-      for (int s = 0; s < nsplit; ++s)
-        a += __builtin_fmaf(p[s * ld + 2] - mean + gl, p[s * ld + 3 + nout + t], p[s * ld + 3 + t]);
-      store_as(out, qi * nout + t, dtype, scale * a);
+    for (int s = threadIdx.x; s < nsplit; s += 256) factor[s] = p[s * ld + 2] - mean + gl;
+    inv = scale;
+    __syncthreads();
+  }
+  const int tt = t < nout ? t : nout - 1;
+  const float* a = p + (GRAD ? 3 : 2) + tt;
+  float v = 0.f;
+  int s = wave;
+  for (; s + 28 < nsplit; s += 32) {
+    float x[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = a[(int64_t)(s + 4 * i) * ld];
+      if (GRAD) y[i] = a[(int64_t)(s + 4 * i) * ld + nout];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (GRAD) v += __builtin_fmaf(factor[s + 4 * i], y[i], x[i]);
+      else v = __builtin_fmaf(x[i], factor[s + 4 * i], v);
     }
   }
+  for (; s < nsplit; s += 4) {
+    const float x = a[(int64_t)s * ld];
+    if (GRAD) v += __builtin_fmaf(factor[s], a[(int64_t)s * ld + nout], x);
+    else v = __builtin_fmaf(x, factor[s], v);
+  }
+  sums[wave][lane] = v;
+  __syncthreads();
+  if (wave == 0 && t < nout) store_as(out, qi * nout + t, dtype, (sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]) * inv);
 }
 
 // q [nq, dk] of any type -> fp32 [nq, d] with zeros behind
@@ -551,6 +1144,27 @@ __global__ __launch_bounds__(256) void attend_pad_kernel(const void* __restrict_
 
 constexpr int kMaxLds = 160 * 1024;
 
+// Which tile kernel serves a call, if any: p->tiles, nq16 (16-query blocks of a tile), nb (64-component runs of the result)
+void tiles_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int dtype, int nprobe, bool grad, AttendPlan* p) {
+  p->tiles = false;
+  if (nprobe > 0 || nq < 2 || ntotal < 64 || g.code_size > 64 || ntotal / g.nlist < 64) return;
+  const int nout = grad ? dk : g.d - v0, planes = dtype == VS_FP32 ? 2 : 1;
+  if (nout > 768) return;
+  p->w = g.dsub <= 2 ? 2 : 4;
+  p->nb = nout <= 128 ? 2 : (nout <= 256 ? 4 : 12);
+  p->nq16 = nq > 16 && p->nb <= 4 ? (grad ? 2 : 4) : 1;   // (what a wavefront's registers hold)
+  p->lds = tile_lds(g, dk, v0, p->w, p->nq16, planes, grad).total;
+  if (p->nq16 > 1 && p->lds > kMaxLds) { p->nq16 = 1; p->lds = tile_lds(g, dk, v0, p->w, 1, planes, grad).total; }
+  if (p->lds > kMaxLds) return;
+  p->tiles = true;
+  p->fits = true;
+  p->qb = 16 * p->nq16;
+  const int64_t groups = (nq + p->qb - 1) / p->qb, want = (512 + groups - 1) / groups;
+  const int64_t most = (ntotal + 255) / 256, splits = want < most ? want : most;
+  p->per = ((ntotal + splits - 1) / splits + 63) / 64 * 64;
+  p->nsplit = (int)((ntotal + p->per - 1) / p->per);
+}
+
 int scan_queries(const IvfpqDims& g, int dk, int v0, int64_t nq, bool probed, bool grad) {
   if (probed || nq == 1) return 1;
   return scan_lds(g, dk, v0, 2, grad).total * 4 <= kMaxLds / 2 ? 2 : 1;
@@ -558,10 +1172,12 @@ int scan_queries(const IvfpqDims& g, int dk, int v0, int64_t nq, bool probed, bo
 
 }  // namespace
 
-AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int nprobe, bool grad) {
-  AttendPlan p;
+AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int dtype, int nprobe, bool grad) {
+  AttendPlan p{};
   p.nout = grad ? dk : g.d - v0;
   p.ld = grad ? 3 + 2 * (int64_t)p.nout : 2 + p.nout;
+  tiles_plan(g, ntotal, nq, dk, v0, dtype, nprobe, grad, &p);
+  if (p.tiles) return p;
   p.qb = scan_queries(g, dk, v0, nq, nprobe > 0, grad);
   p.lds = scan_lds(g, dk, v0, p.qb, grad).total * 4;
   p.fits = p.lds <= kMaxLds;
@@ -594,8 +1210,27 @@ void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* p
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
     kern<<<g, 256, p.lds, st>>>(a);
   };
-  if (grad) { if (p.qb == 2) run(attend_scan_kernel<2, true>); else run(attend_scan_kernel<1, true>); }
+  if (p.tiles) {
+#define TILES(W, NQ, NB)                                                        \
+  do {                                                                          \
+    constexpr int NG = NQ == 4 ? 2 : 1;                                         \
+    if (c.dtype == VS_FP32) { if (grad) run(attend_tiles_kernel<W, NG, NB, 2, true>); else run(attend_tiles_kernel<W, NQ, NB, 2, false>); } \
+    else { if (grad) run(attend_tiles_kernel<W, NG, NB, 1, true>); else run(attend_tiles_kernel<W, NQ, NB, 1, false>); } \
+  } while (0)
+#define TILES_W(W)                                                              \
+  do {                                                                          \
+    if (p.nq16 > 1) { if (p.nb == 2) TILES(W, 4, 2); else TILES(W, 4, 4); }     \
+    else if (p.nb == 2) TILES(W, 1, 2);                                          \
+    else if (p.nb == 4) TILES(W, 1, 4);                                          \
+    else TILES(W, 1, 12);                                                        \
+  } while (0)
+    if (p.w == 2) TILES_W(2);
+    else TILES_W(4);
+#undef TILES_W
+#undef TILES
+  } else if (grad) { if (p.qb == 2) run(attend_scan_kernel<2, true>); else run(attend_scan_kernel<1, true>); }
   else { if (p.qb == 2) run(attend_scan_kernel<2, false>); else run(attend_scan_kernel<1, false>); }
-  if (grad) attend_join_kernel<true><<<(unsigned)c.nq, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, c.g_lse, c.scale, c.dtype, c.out, nullptr);
-  else attend_join_kernel<false><<<(unsigned)c.nq, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, nullptr, c.scale, c.dtype, c.out, c.out_lse);
+  const dim3 gj((unsigned)c.nq, (unsigned)((p.nout + 63) / 64));
+  if (grad) attend_join_kernel<true><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, c.g_lse, c.scale, c.dtype, c.out, nullptr);
+  else attend_join_kernel<false><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, nullptr, c.scale, c.dtype, c.out, c.out_lse);
 }

@@ -92,8 +92,10 @@ struct AttendPlan {
   int qb, nsplit, nout, lds;                     // queries a workgroup takes; parts of their rows; results; bytes of LDS
   int64_t per, ld;                               // rows (probes) of a part; floats of a partial result
   bool fits;
+  bool tiles;                                    // decoded tiles on the matrix cores, in pieces of w components,
+  int w, nq16, nb;                               // 16 nq16 queries and up to 64 nb results a workgroup
 };
-AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int nprobe, bool grad);
+AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int dtype, int nprobe, bool grad);
 void launch_attend_pad(const void* q, int64_t nq, int dk, int d, int dtype, float* out, hipStream_t st);
 // part: [nq][nsplit][ld] floats of scratch
 void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* part, hipStream_t st);

@@ -167,7 +167,7 @@ int attend_space(const char* who, const vs_ivfpq* ix, int64_t nq, int dk, int v0
   if (v0 < 0 || v0 >= s.g.d || v0 % s.g.dsub) return fail(VS_ERR_INVALID_ARG, "%s: v0 = %d is not a multiple of %d in [0, %d)", who, v0, s.g.dsub, s.g.d);
   if (nprobe < 0 || nprobe > VS_MAX_K) return fail(VS_ERR_INVALID_ARG, "%s: nprobe = %d outside [0, %d]", who, nprobe, VS_MAX_K);
   o->nprobe = nprobe < s.g.nlist ? nprobe : 0;
-  o->plan = attend_plan(s.g, s.ntotal, nq, dk, v0, o->nprobe, grad);
+  o->plan = attend_plan(s.g, s.ntotal, nq, dk, v0, dtype, o->nprobe, grad);
   if (!o->plan.fits) return fail(VS_ERR_UNSUPPORTED, "%s: the tables of M = %d, d = %d exceed the on-chip memory", who, s.g.M, s.g.d);
   if ((nq + o->plan.qb - 1) / o->plan.qb * o->plan.nsplit >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 workgroups", who);
   Carver c;
