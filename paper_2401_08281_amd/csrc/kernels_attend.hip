@@ -21,10 +21,6 @@ constexpr int kSegments = 64;       // lists it may span
 constexpr int kWaves = 4;
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
-typedef __attribute__((address_space(3))) float* lds_float;
-__device__ __forceinline__ void lds_add(float* p, float v) {
-  __builtin_amdgcn_ds_faddf((lds_float)p, v, 0, 0, false);
-}
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
@@ -430,10 +426,10 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
 #pragma unroll
               for (int b = 0; b < QB; ++b) {
                 if (GRAD) {
-                  lds_add(hc + (0 * QB + b) * L.mc * 1024 + c * 64, pr2[j * QB + b]);
-                  lds_add(hc + (1 * QB + b) * L.mc * 1024 + c * 64, pr[j * QB + b]);
+                  hc[(0 * QB + b) * L.mc * 1024 + c * 64] += pr2[j * QB + b];
+                  hc[(1 * QB + b) * L.mc * 1024 + c * 64] += pr[j * QB + b];
                 } else {
-                  lds_add(hc + b * L.mc * 1024 + c * 64, pr[j * QB + b]);
+                  hc[b * L.mc * 1024 + c * 64] += pr[j * QB + b];
                 }
               }
             }

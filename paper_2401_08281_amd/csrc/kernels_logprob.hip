@@ -864,29 +864,98 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
   }
 }
 
+// ---- long products -------------------------------------------------------------------------
+// out[b][a] = sum_k A[a][k] B[b][k] over long K: tiles of 256 x 256, eight wavefronts of 128 x 64 each.  Against 128 x 128
+// tiles a K block reads three quarters of the LDS per product, and its 2048 cycles of products a SIMD cover the way of the
+// next block from the last-level cache.  Fragments of the next 16 K elements are read while the present ones multiply.
+constexpr int kBigTile = 256;
+constexpr int kBigStage = 2 * kBigTile * 128;
 template <int PLANES>
-__global__ __launch_bounds__(256, 2) void sm_product_kernel(SmMatrix A, SmMatrix B, int64_t kblocks, int splits, int add,
+__global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix B, int64_t kblocks, int splits, int add,
                                                             float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   const int64_t tiles = ta * tb;
   const int split = (int)(blockIdx.x / tiles);
   tile_of(blockIdx.x - split * tiles, ta, tb, &ia, &ib_);
-  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
+  const int64_t a0 = ia * kBigTile, b0 = ib_ * kBigTile;
   const int64_t k0 = kblocks * split / splits, k1 = kblocks * (split + 1) / splits;
-  f32x16 acc[2][2] = {};
-  if (k1 > k0) TileMul<PLANES, false>::run(A, a0, B, b0, k0, k1, lds, acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  f32x16 acc[4][2] = {};
+  const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
+  const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
+  const int ra_max = (int)(A.rows - 1 - a0 < kBigTile ? A.rows - 1 - a0 : kBigTile - 1);
+  const int rb_max = (int)(B.rows - 1 - b0 < kBigTile ? B.rows - 1 - b0 : kBigTile - 1);
+  const char* ga[4];
+  const char* gb[4];
+  const int piece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = (wave * 4 + i) * 8 + (lane >> 3);
+    ga[i] = pa + (int64_t)(r < ra_max ? r : ra_max) * A.row_bytes + k0 * 128 + piece * 16;
+    gb[i] = pb + (int64_t)(r < rb_max ? r : rb_max) * B.row_bytes + k0 * 128 + piece * 16;
+  }
+  auto request = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ga[i],
+                                       (__attribute__((address_space(3))) void*)(lds + stage * kBigStage + (wave * 4 + i) * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)gb[i],
+                                       (__attribute__((address_space(3))) void*)(lds + stage * kBigStage + kBigStage / 2 + (wave * 4 + i) * 1024), 16, 0, 0);
+      ga[i] += 128;
+      gb[i] += 128;
+    }
+  };
+  const int ra = (wa * 128 + (lane & 31)) * 128, rb = (wb * 64 + (lane & 31)) * 128, sw = lane & 7;
+  const int n = (int)(k1 - k0);
+  if (n > 0) request(0);
+  for (int t = 0; t < n; ++t) {
+    __syncthreads();                                  // the stage has landed, the other one is free
+    if (t + 1 < n) request((t + 1) & 1);
+    const char* s = lds + (t & 1) * kBigStage;
+    u32x4 a[2][4], b[2][2];
+    auto fragments = [&](int ks, u32x4 (&fa)[4], u32x4 (&fb)[2]) {
+      const int off = ((2 * ks + half) ^ sw) * 16;
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) fa[ib] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 128 + off);
+#pragma unroll
+      for (int jb = 0; jb < 2; ++jb) fb[jb] = *reinterpret_cast<const u32x4*>(s + kBigStage / 2 + rb + jb * 32 * 128 + off);
+    };
+    auto products = [&](const u32x4 (&fa)[4], const u32x4 (&fb)[2]) {
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib)
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) acc[ib][jb] = TileMul<PLANES, false>::mul(fa[ib], fb[jb], acc[ib][jb]);
+    };
+    if constexpr (PLANES == 1) {
+      fragments(0, a[0], b[0]);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        if (ks < 3) fragments(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
+        products(a[ks & 1], b[ks & 1]);
+      }
+    } else {                                          // heads 0, 1 and tails 2, 3: hi hi + hi lo + lo hi
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        fragments(ks, a[0], b[0]);
+        fragments(ks + 2, a[1], b[1]);
+        products(a[0], b[0]);
+        products(a[0], b[1]);
+        products(a[1], b[0]);
+      }
+    }
+  }
+  settle_products();
 #pragma unroll
   for (int jb = 0; jb < 2; ++jb) {
     const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
     if (b >= B.rows) continue;
     float* out = part + (split * B.rows + b) * ld;
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int64_t a = a0 + wa * 64 + ib * 32 + 2 * r + 4 * half;
+        const int64_t a = a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;
         if (a >= ld) continue;                                      // (ld is a multiple of 4 and at least A.rows)
         float4 v = make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
         float4* o = reinterpret_cast<float4*>(out + a);
@@ -1038,10 +1107,14 @@ void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const 
 
 void launch_sm_product(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, int splits, bool add,
                        float* part, int64_t ld, hipStream_t st) {
-  const int64_t ta = tiles(A.rows), tb = tiles(B.rows);
+  const int64_t ta = (A.rows + kBigTile - 1) / kBigTile, tb = (B.rows + kBigTile - 1) / kBigTile;
   const unsigned g = (unsigned)(ta * tb * splits);
-  if (f.planes == 2) sm_product_kernel<2><<<g, 256, kTileLds, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
-  else sm_product_kernel<1><<<g, 256, kTileLds, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
+  auto run = [&](auto kern) {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBigStage);
+    kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
+  };
+  if (f.planes == 2) run(sm_product_kernel<2>);
+  else run(sm_product_kernel<1>);
 }
 
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* sa, const float* sb,

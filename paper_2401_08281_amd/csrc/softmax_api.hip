@@ -86,9 +86,10 @@ struct GradPlan {
   int64_t o_x, o_xs, o_q, o_qs, o_xt, o_xts, o_qt, o_qts, o_cm, o_coef, o_bound, o_g, o_gt, o_dq, o_dx, o_db, bytes;
 };
 
-// Workgroups that a product should have: two a CU.  Fewer tiles than that share their K blocks out, 8 blocks each at least.
-int product_splits(int64_t tiles, int64_t kblocks) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({16, (512 + tiles - 1) / tiles, kblocks / 8}));
+// Workgroups that a product should have: one a CU.  Fewer tiles than that share their K blocks out, 8 blocks each at least.
+int product_splits(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
+  const int64_t tiles = (rows_a + 255) / 256 * ((rows_b + 255) / 256);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({16, (256 + tiles / 2) / tiles, kblocks / 8}));
 }
 
 GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
@@ -105,9 +106,8 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   p.gt_row = nqp * el;
   p.xt_row = p.f.blocks(nb) * 128;
   p.qt_row = p.f.blocks(nq) * 128;
-  const int64_t td = round_up(d, kSmTile) / kSmTile;
-  p.splits_q = product_splits(td * (nqp / kSmTile), p.f.blocks(p.chunk));
-  p.splits_x = product_splits(td * (p.chunk / kSmTile), p.f.blocks(nq));
+  p.splits_q = product_splits(d, nq, p.f.blocks(p.chunk));
+  p.splits_x = product_splits(d, p.chunk, p.f.blocks(nq));
   Carver c;
   if (!p.direct) {
     p.o_x = c.take(nb * p.row_bytes);
