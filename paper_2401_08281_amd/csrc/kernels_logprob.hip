@@ -56,11 +56,15 @@ __device__ __forceinline__ void settle_products() {
 }
 
 // ---- tiles -------------------------------------------------------------------------
-// One K block (128 bytes) of 128 rows of each operand is a stage of 2 x 16 KB; two stages alternate, the next is
-// requested straight into LDS (global_load_lds_dwordx4) before the products of the present one.  A row's eight 16-byte
-// pieces are stored at piece ^ (row & 7): a fragment read (32 rows x 2 pieces) then touches every bank evenly.
-// With two planes a block holds 32 heads and their 32 tails, and one stage feeds hi*hi + hi*lo + lo*hi.
-constexpr int kStage = 2 * kSmTile * 128;
+// A workgroup of four wavefronts takes 256 rows by 128 queries, a wavefront 128 x 64 of them: 12 fragment reads from LDS
+// feed 16 products (64 x 64 needs 16).  One K unit (64 bytes) of the 384 operand rows is a stage of 24 KB; two stages
+// alternate, the next is requested straight into LDS (global_load_lds_dwordx4) before the products of the present one,
+// and two workgroups a CU fill each other's waits and run one's epilogue beside the other's products.  A row's four 16-byte
+// pieces are stored at piece ^ ((row >> 2) & 3): a fragment read (32 rows x 2 pieces) then touches every bank evenly.
+// With two planes a unit holds 16 heads and their 16 tails, and one stage feeds hi*hi + hi*lo + lo*hi.
+// Against tiles of 128 x 128 by 64 x 64 (K units of 128 bytes), scores of 4096 x 65,536 x 768: measured beside the kernel.
+constexpr int kTileA = 256, kTileB = 128;
+constexpr int kStage = (kTileA + kTileB) * 64;
 constexpr int kTileLds = 2 * kStage;
 
 template <int PLANES, bool BF16>
@@ -71,65 +75,73 @@ struct TileMul {
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
-  // acc[ib][jb] of this wavefront: rows 64 wa + 32 ib .., queries 64 wb + 32 jb ..
-  static __device__ __forceinline__ void run(const SmMatrix& A, int64_t a0, const SmMatrix& B, int64_t b0, int64_t kb0,
-                                             int64_t kb1, char* lds, f32x16 (&acc)[2][2]) {
+  // acc[ib][jb] of this wavefront: rows 128 wa + 32 ib .., queries 64 wb + 32 jb ..; K units [ku0, ku1), at least one
+  static __device__ __forceinline__ void run(const SmMatrix& A, int64_t a0, const SmMatrix& B, int64_t b0, int64_t ku0,
+                                             int64_t ku1, char* lds, f32x16 (&acc)[4][2]) {
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     const int wa = wave & 1, wb = wave >> 1;
     // rows past the last one repeat it: their results are dropped
     const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
     const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
-    const int ra_max = (int)(A.rows - 1 - a0 < kSmTile ? A.rows - 1 - a0 : kSmTile - 1);
-    const int rb_max = (int)(B.rows - 1 - b0 < kSmTile ? B.rows - 1 - b0 : kSmTile - 1);
+    const int ra_max = (int)(A.rows - 1 - a0 < kTileA ? A.rows - 1 - a0 : kTileA - 1);
+    const int rb_max = (int)(B.rows - 1 - b0 < kTileB ? B.rows - 1 - b0 : kTileB - 1);
     const char* ga[4];
-    const char* gb[4];
-    const int piece = (lane & 7) ^ (lane >> 3);
+    const char* gb[2];
+    const int piece = (lane & 3) ^ ((lane >> 4) & 3);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = (wave * 4 + i) * 8 + (lane >> 3);
-      ga[i] = pa + (int64_t)(r < ra_max ? r : ra_max) * A.row_bytes + kb0 * 128 + piece * 16;
-      gb[i] = pb + (int64_t)(r < rb_max ? r : rb_max) * B.row_bytes + kb0 * 128 + piece * 16;
+      const int r = (wave * 4 + i) * 16 + (lane >> 2);
+      ga[i] = pa + (int64_t)(r < ra_max ? r : ra_max) * A.row_bytes + ku0 * 64 + piece * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = (wave * 2 + i) * 16 + (lane >> 2);
+      gb[i] = pb + (int64_t)(r < rb_max ? r : rb_max) * B.row_bytes + ku0 * 64 + piece * 16;
     }
     auto request = [&](int stage) {
+      char* to = lds + stage * kStage;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ga[i],
-                                         (__attribute__((address_space(3))) void*)(lds + stage * kStage + (wave * 4 + i) * 1024), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(to + (wave * 4 + i) * 1024), 16, 0, 0);
+        ga[i] += 64;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)gb[i],
-                                         (__attribute__((address_space(3))) void*)(lds + stage * kStage + kStage / 2 + (wave * 4 + i) * 1024), 16, 0, 0);
-        ga[i] += 128;
-        gb[i] += 128;
+                                         (__attribute__((address_space(3))) void*)(to + kTileA * 64 + (wave * 2 + i) * 1024), 16, 0, 0);
+        gb[i] += 64;
       }
     };
-    const int ra = (wa * 64 + (lane & 31)) * 128, rb = (wb * 64 + (lane & 31)) * 128, half = lane >> 5, sw = lane & 7;
+    const int ra = (wa * 128 + (lane & 31)) * 64, rb = kTileA * 64 + (wb * 64 + (lane & 31)) * 64, half = lane >> 5, sw = (lane >> 2) & 3;
     request(0);
-    const int n = (int)(kb1 - kb0);
+    const int n = (int)(ku1 - ku0);
     for (int t = 0; t < n; ++t) {
       __syncthreads();                                  // the stage has landed, the other one is free
       const char* s = lds + (t & 1) * kStage;
-      u32x4 a[2][4], b[2][4];
+      u32x4 a[2][4], b[2][2];
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
+      for (int ks = 0; ks < 2; ++ks) {
         const int off = ((2 * ks + half) ^ sw) * 16;
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib) {
-          a[ib][ks] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 128 + off);
-          b[ib][ks] = *reinterpret_cast<const u32x4*>(s + kStage / 2 + rb + ib * 32 * 128 + off);
-        }
+        for (int ib = 0; ib < 4; ++ib) a[ks][ib] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 64 + off);
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) b[ks][jb] = *reinterpret_cast<const u32x4*>(s + rb + jb * 32 * 64 + off);
       }
       if (t + 1 < n) request((t + 1) & 1);
+      auto products = [&](const u32x4 (&fa)[4], const u32x4 (&fb)[2]) {
 #pragma unroll
-      for (int ks = 0; ks < (PLANES == 2 ? 2 : 4); ++ks)
+        for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-          for (int jb = 0; jb < 2; ++jb) {
-            acc[ib][jb] = mul(a[ib][ks], b[jb][ks], acc[ib][jb]);
-            if constexpr (PLANES == 2) {
-              acc[ib][jb] = mul(a[ib][ks], b[jb][ks + 2], acc[ib][jb]);
-              acc[ib][jb] = mul(a[ib][ks + 2], b[jb][ks], acc[ib][jb]);
-            }
-          }
+          for (int jb = 0; jb < 2; ++jb) acc[ib][jb] = mul(fa[ib], fb[jb], acc[ib][jb]);
+      };
+      products(a[0], b[0]);
+      if constexpr (PLANES == 1) {
+        products(a[1], b[1]);
+      } else {
+        products(a[0], b[1]);
+        products(a[1], b[0]);
+      }
     }
     __syncthreads();                                    // LDS is free for the epilogue
   }
@@ -176,130 +188,98 @@ __device__ __forceinline__ Best join_mixed(Best a, Best b) {
 
 // The scores of a wavefront's tile in place of its products: s = acc * (row factor * query factor) + bias, -inf for
 // rows that do not exist (past the end, or bias -inf: whatever their products are).
-// rowdata: LDS, {row factor, bias} of the workgroup's 128 rows, filled here.
-__device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[2][2]) {
+// rowdata: LDS, {row factor, bias} of the workgroup's 256 rows, filled here.
+__device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[4][2]) {
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1;
-  const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + kSmTile <= S.nx;   // (the same in the workgroup)
+  const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + kTileA <= S.nx;   // (the same in the workgroup)
   if (!plain) {
-    if (threadIdx.x < kSmTile) {
-      const int64_t j = a0 + threadIdx.x;
-      const bool in = j < S.nx;
-      rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
-    }
+    const int64_t j = a0 + threadIdx.x;
+    const bool in = j < S.nx;
+    rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
     __syncthreads();
   }
+  float cq[2];
 #pragma unroll
   for (int jb = 0; jb < 2; ++jb) {
     const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
-    const float cq = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] : 1.f);
+    cq[jb] = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] : 1.f);
+  }
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+  for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (plain) {
-          acc[ib][jb][r] *= cq;
-        } else {
-          const float2 rd = rowdata[wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)];
-          const float s = acc[ib][jb][r] * rd.x * cq + rd.y;
+    for (int r = 0; r < 16; ++r) {
+      if (plain) {
+        acc[ib][0][r] *= cq[0];
+        acc[ib][1][r] *= cq[1];
+      } else {
+        const float2 rd = rowdata[wa * 128 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)];
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+          const float s = acc[ib][jb][r] * rd.x * cq[jb] + rd.y;
           acc[ib][jb][r] = rd.y == neg_inf() ? neg_inf() : s;
         }
       }
-  }
+    }
 }
 
 // ---- forward: scores -> softmax records ---------------------------------------------
 // Bound by the matrix cores for long vectors and by the epilogue's exponentials (some 12 vector instructions per score)
-// for short ones; two workgroups per CU let one's epilogue run beside the other's products.
+// for short ones.  A wavefront's 128 rows are a record of each of its 64 queries.
 template <int PLANES, bool BF16, bool SECOND>
 __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords R, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   tile_of(blockIdx.x, ta, tb, &ia, &ib_);
-  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
-  f32x16 acc[2][2] = {};
-  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kblocks, lds, acc);
-  float2* rowdata = reinterpret_cast<float2*>(lds);
-  finish_scores(S, a0, b0, rowdata, acc);
+  const int64_t a0 = ia * kTileA, b0 = ib_ * kTileB;
+  f32x16 acc[4][2] = {};
+  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
+  finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
-  float4* other = reinterpret_cast<float4*>(lds + 1024);            // [128] records of the second 64 rows
-  float* other_second = reinterpret_cast<float*>(lds + 1024 + 2048);
-  float mx[2], sum[2], ent[2];
-  Best best[2];
 #pragma unroll
   for (int jb = 0; jb < 2; ++jb) {
+    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
     float m = neg_inf(), second = neg_inf();
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float s = acc[ib][jb][r];
         if (SECOND) second = __builtin_amdgcn_fmed3f(s, m, second);
         m = fmaxf(m, s);
       }
-    int pos = 0;
+    float w = 0.f;
     if (SECOND) {
+      int pos = 0;
 #pragma unroll
-      for (int ib = 1; ib >= 0; --ib)
+      for (int ib = 3; ib >= 0; --ib)
 #pragma unroll
         for (int r = 15; r >= 0; --r)
-          pos = acc[ib][jb][r] == m ? wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half : pos;
-      Best mine{m, second, pos};
-      Best theirs{__shfl_xor(m, 32), __shfl_xor(second, 32), __shfl_xor(pos, 32)};
-      best[jb] = join_mixed(mine, theirs);
-      m = best[jb].m;
+          pos = acc[ib][jb][r] == m ? ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half : pos;
+      const Best b = join_mixed(Best{m, second, pos}, Best{__shfl_xor(m, 32), __shfl_xor(second, 32), __shfl_xor(pos, 32)});
+      m = b.m;
+      w = pack_second(b.second, b.pos);
     } else {
       m = fmaxf(m, __shfl_xor(m, 32));
     }
     float l = 0.f, h = 0.f;
     const float base = m > neg_inf() ? m : 0.f;
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) softmax_add(acc[ib][jb][r] - base, &l, &h);
     l += __shfl_xor(l, 32);
     h += __shfl_xor(h, 32);
-    mx[jb] = m; sum[jb] = l; ent[jb] = h;
-    if (R.keep) {
-      const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
-      if (qi < S.nq)
+    if (R.keep && qi < S.nq)
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
+      for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            const int64_t j = a0 + wa * 64 + ib * 32 + 8 * (r >> 2) + 4 * half;   // keep_ld is a multiple of 128: no tail
-            *reinterpret_cast<float4*>(R.keep + qi * R.keep_ld + j) =
-                make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
-          }
-    }
-  }
-  __syncthreads();                                                  // (rowdata has been read)
-  if (wa == 1 && half == 0) {
-#pragma unroll
-    for (int jb = 0; jb < 2; ++jb) {
-      const int c = wb * 64 + jb * 32 + (lane & 31);
-      other[c] = make_float4(mx[jb], sum[jb], ent[jb], SECOND ? __int_as_float(best[jb].pos) : 0.f);
-      if (SECOND) other_second[c] = best[jb].second;
-    }
-  }
-  __syncthreads();
-  if (wa == 0 && half == 0) {
-#pragma unroll
-    for (int jb = 0; jb < 2; ++jb) {
-      const int c = wb * 64 + jb * 32 + (lane & 31);
-      const int64_t qi = b0 + c;
-      if (qi >= S.nq) continue;
-      const float4 o = other[c];
-      const float m = fmaxf(mx[jb], o.x);
-      float l = 0.f, h = 0.f;
-      softmax_join(m, mx[jb], sum[jb], ent[jb], &l, &h);
-      softmax_join(m, o.x, o.y, o.z, &l, &h);
-      float w = 0.f;
-      if (SECOND) {
-        const Best b = join_best(best[jb], Best{o.x, other_second[c], __float_as_int(o.w)});
-        w = pack_second(b.second, b.pos);
-      }
-      R.rec[qi * R.parts + ia] = make_float4(m, l, h, w);
-    }
+        for (int r = 0; r < 16; r += 4) {
+          const int64_t j = a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;   // keep_ld covers whole tiles: no tail
+          *reinterpret_cast<float4*>(R.keep + qi * R.keep_ld + j) =
+              make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
+        }
+    const int64_t part = ia * 2 + wa;
+    if (half == 0 && qi < S.nq && part < R.parts) R.rec[qi * R.parts + part] = make_float4(m, l, h, w);
   }
 }
 
@@ -638,9 +618,9 @@ __device__ __forceinline__ void put_planes(char* row, int64_t k, float v) {
   if (PLANES == 1) {
     reinterpret_cast<_Float16*>(row)[k] = hi;
   } else {
-    _Float16* b = reinterpret_cast<_Float16*>(row + (k >> 5) * 128) + (k & 31);
+    _Float16* b = reinterpret_cast<_Float16*>(row + (k >> 4) * 64) + (k & 15);
     b[0] = hi;
-    b[32] = (_Float16)(v - (float)hi);
+    b[16] = (_Float16)(v - (float)hi);
   }
 }
 
@@ -664,48 +644,96 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<D
   if (lane == 0) scale[r] = down;
 }
 
+// Elements k .. k + 15 / sizeof(T) of a row as floats, zeros past its end (vec: rows of whole 16-byte pieces)
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int d, bool vec, float (&v)[16 / sizeof(T)]) {
+  constexpr int V = 16 / sizeof(T);
+  if (vec && k < d) {
+    T e[V];
+    __builtin_memcpy(e, row + k, 16);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = to_f32(e[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = k + i < d ? to_f32(row[k + i]) : 0.f;
+  }
+}
+
+// Largest size in every column: a thread goes down 16 bytes of columns.  (A maximum does not depend on the order, and
+// non-negative floats are ordered as their bits.)
 template <int DT>
 __global__ __launch_bounds__(256) void sm_colmax_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
                                                         const float* __restrict__ bias, const float* __restrict__ factor,
                                                         int64_t rows_per, u32* __restrict__ colmax) {
-  const int t = blockIdx.x * 64 + (threadIdx.x & 63);
+  typedef typename Elem<DT>::T T;
+  constexpr int V = 16 / sizeof(T);
+  __shared__ float part[4][64 * V];
+  const int lane = lane_id(), wave = threadIdx.x >> 6, t = (blockIdx.x * 64 + lane) * V;
+  const bool vec = d % V == 0;
   const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < n ? r0 + rows_per : n;
-  float mx = 0.f;
+  float mx[V] = {};
   if (t < d)
-    for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += 4) {
+#pragma unroll 4
+    for (int64_t r = r0 + wave; r < r1; r += 4) {
       const float f = bias && bias[r] == neg_inf() ? 0.f : (factor ? factor[r] : 1.f);
-      if (f != 0.f) mx = fmaxf(mx, fabsf(to_f32(x[r * d + t])) * f);
+      float v[V];
+      load_piece(x + r * d, t, d, vec, v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) mx[i] = f != 0.f ? fmaxf(mx[i], fabsf(v[i]) * f) : mx[i];
     }
-  // (a maximum does not depend on the order; non-negative floats are ordered as their bits)
-  if (t < d && mx > 0.f) atomicMax(colmax + t, __float_as_uint(mx));
+#pragma unroll
+  for (int i = 0; i < V; ++i) part[wave][lane * V + i] = mx[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 64 * V; i += 256) {
+    const float m = fmaxf(fmaxf(part[0][i], part[1][i]), fmaxf(part[2][i], part[3][i]));
+    const int c = blockIdx.x * 64 * V + i;
+    if (c < d && m > 0.f) atomicMax(colmax + c, __float_as_uint(m));
+  }
 }
 
-// 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r
+// 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r, read and written in 16-byte pieces
 template <int DT, int PLANES>
 __global__ __launch_bounds__(256) void sm_prep_cols_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
                                                            int64_t np, const float* __restrict__ bias,
                                                            const float* __restrict__ factor, const u32* __restrict__ colmax,
                                                            char* __restrict__ planes, float* __restrict__ scale) {
+  typedef typename Elem<DT>::T T;
+  constexpr int V = 16 / sizeof(T);
   __shared__ float tile[64][65];
   const int64_t r0 = (int64_t)blockIdx.x * 64;
-  const int t0 = blockIdx.y * 64, lane = lane_id(), wave = threadIdx.x >> 6;
-  for (int i = wave; i < 64; i += 4) {
-    const int64_t r = r0 + i;
-    float v = 0.f;
-    if (r < n && t0 + lane < d) {
-      const float f = bias && bias[r] == neg_inf() ? 0.f : (factor ? factor[r] : 1.f);
-      if (f != 0.f) v = to_f32(x[r * d + t0 + lane]) * f;          // (what takes no part is not read)
-    }
-    tile[i][lane] = v;
+  const int t0 = blockIdx.y * 64;
+  const bool vec = d % V == 0;
+  for (int i = threadIdx.x; i < 64 * 64 / V; i += 256) {
+    const int row = i / (64 / V), c = i % (64 / V) * V;
+    const int64_t r = r0 + row;
+    float v[V] = {};
+    const float f = r < n && !(bias && bias[r] == neg_inf()) ? (factor ? factor[r] : 1.f) : 0.f;
+    if (f != 0.f && t0 + c < d) load_piece(x + r * d, t0 + c, d, vec, v);
+#pragma unroll
+    for (int u = 0; u < V; ++u) tile[row][c + u] = f != 0.f ? v[u] * f : 0.f;   // (what takes no part may be a NaN)
   }
   __syncthreads();
-  for (int i = wave; i < 64; i += 4) {
-    const int t = t0 + i;
-    if (t >= d) break;
+  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+    const int c = i & 63, k = (i >> 6) * 8, t = t0 + c;
+    if (t >= d || r0 + k >= np) continue;
     float up, down;
     row_scale(__uint_as_float(colmax[t]), &up, &down);
-    if (r0 + lane < np) put_planes<PLANES>(planes + (int64_t)t * (np * 2 * PLANES), r0 + lane, tile[lane][i] * up);
-    if (blockIdx.x == 0 && lane == 0) scale[t] = down;
+    f16x8 hi, lo;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float v = tile[k + u][c] * up;
+      hi[u] = (_Float16)v;
+      lo[u] = (_Float16)(v - (float)hi[u]);
+    }
+    char* out = planes + (int64_t)t * (np * 2 * PLANES);
+    const int64_t kk = r0 + k;
+    if (PLANES == 1) {
+      *reinterpret_cast<f16x8*>(out + kk * 2) = hi;
+    } else {
+      *reinterpret_cast<f16x8*>(out + (kk >> 4) * 64 + (kk & 15) * 2) = hi;
+      *reinterpret_cast<f16x8*>(out + (kk >> 4) * 64 + 32 + (kk & 15) * 2) = lo;
+    }
+    if (blockIdx.x == 0 && k == 0) scale[t] = down;
   }
 }
 
@@ -741,9 +769,9 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   tile_of(blockIdx.x, ta, tb, &ia, &ib_);
-  const int64_t a0 = ia * kSmTile, b0 = ib_ * kSmTile;
-  f32x16 acc[2][2] = {};
-  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kblocks, lds, acc);
+  const int64_t a0 = ia * kTileA, b0 = ib_ * kTileB;
+  f32x16 acc[4][2] = {};
+  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
   finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
@@ -753,7 +781,7 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
     const float4 c = in ? O.coef[qi] : make_float4(0.f, 0.f, 0.f, neg_inf());
     const bool some = c.w != neg_inf();
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float s = acc[ib][jb][r];
@@ -764,26 +792,26 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
       }
     if (O.g_logp && in)
       for (int t = 0; t < O.nt; ++t) {
-        const int64_t j = O.targets[qi * O.nt + t] - O.row0 - a0 - wa * 64;   // relative to the wavefront's rows
-        if (j >= 0 && j < 64) {
+        const int64_t j = O.targets[qi * O.nt + t] - O.row0 - a0 - wa * 128;  // relative to the wavefront's rows
+        if (j >= 0 && j < 128) {
           const float gl = O.g_logp[qi * O.nt + t];
 #pragma unroll
-          for (int ib = 0; ib < 2; ++ib)
+          for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if ((int)j == ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) acc[ib][jb][r] += gl;
         }
       }
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[ib][jb][r] = acc[ib][jb][r] == neg_inf() ? 0.f : acc[ib][jb][r];
   }
   __syncthreads();                                                  // (rowdata has been read)
   if (O.db) {                                                       // column sums of this tile, in a fixed order
-    float* dbs = reinterpret_cast<float*>(lds);                     // [2][128]
+    float* dbs = reinterpret_cast<float*>(lds);                     // [2][256]
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         float v = acc[ib][0][r] + acc[ib][1][r];
@@ -792,11 +820,10 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
         v += __uint_as_float(lane_xor_u32<4>(__float_as_uint(v)));
         v += __uint_as_float(lane_xor_u32<8>(__float_as_uint(v)));
         v += __shfl_xor(v, 16);
-        if ((lane & 31) == 0) dbs[wb * 128 + wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half] = v;
+        if ((lane & 31) == 0) dbs[wb * 256 + wa * 128 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half] = v;
       }
     __syncthreads();
-    if (threadIdx.x < 128 && a0 + threadIdx.x < S.nx)
-      O.db[ib_ * O.db_ld + a0 + threadIdx.x] = dbs[threadIdx.x] + dbs[128 + threadIdx.x];
+    if (a0 + threadIdx.x < S.nx) O.db[ib_ * O.db_ld + a0 + threadIdx.x] = dbs[threadIdx.x] + dbs[256 + threadIdx.x];
     __syncthreads();
   }
 #pragma unroll
@@ -805,63 +832,90 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
     const float bnd = qi < S.nq ? O.bound[qi] : 0.f;
     const float inv = bnd == 0.f ? 0.f : 16384.f / bnd;
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib)
+    for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[ib][jb][r] *= inv;
   }
-  constexpr int LD = 2 * kSmTile + 16;                              // bytes of a row of the staged tile
-  constexpr int PER = PLANES == 2 ? 32 : 64;                        // elements of a K block
+  // Out through LDS, 128 rows by 128 queries at a time: the wavefronts of one half of the rows write, all copy.
+  constexpr int LD = 2 * 128 + 16;                                  // bytes of a row of the staged tile
+  constexpr int PER = PLANES == 2 ? 16 : 32;                        // elements of a K unit
   for (int plane = 0; plane < PLANES; ++plane) {
-    if (O.g) {
-      // rows of G: queries; four consecutive rows of x are 8 bytes of it
+    for (int h = 0; h < 2; ++h) {
+      const int64_t x0 = a0 + h * 128;
+      if (O.g) {
+        // rows of G: queries; four consecutive rows of x are 8 bytes of it
+        if (wa == h) {
 #pragma unroll
-      for (int jb = 0; jb < 2; ++jb)
+          for (int jb = 0; jb < 2; ++jb)
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
+            for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            f16x4 v;
+              for (int r = 0; r < 16; r += 4) {
+                f16x4 v;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) v[u] = (_Float16)acc[ib][jb][r + u];
-            *reinterpret_cast<f16x4*>(lds + (wb * 64 + jb * 32 + (lane & 31)) * LD +
-                                      2 * (wa * 64 + ib * 32 + 2 * r + 4 * half)) = v;
-          }
-      __syncthreads();
-      for (int i = threadIdx.x; i < kSmTile * 16; i += 256) {
-        const int row = i >> 4, k = (i & 15) * 8;                   // 8 elements
-        if (b0 + row < S.nq)
-          *reinterpret_cast<u32x4*>(static_cast<char*>(O.g) + (b0 + row) * O.g_row_bytes + (a0 + k) / PER * 128 + plane * 64 +
-                                    (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+                for (int u = 0; u < 4; ++u) v[u] = (_Float16)acc[ib][jb][r + u];
+                *reinterpret_cast<f16x4*>(lds + (wb * 64 + jb * 32 + (lane & 31)) * LD + 2 * (ib * 32 + 2 * r + 4 * half)) = v;
+              }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 128 * 16; i += 256) {
+          const int row = i >> 4, k = (i & 15) * 8;                 // 8 elements
+          if (b0 + row < S.nq)
+            *reinterpret_cast<u32x4*>(static_cast<char*>(O.g) + (b0 + row) * O.g_row_bytes + (x0 + k) / PER * 64 + plane * 32 +
+                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+        }
+        __syncthreads();
       }
-      __syncthreads();
-    }
-    if (O.gt) {
+      if (O.gt) {
+        if (wa == h) {
 #pragma unroll
-      for (int jb = 0; jb < 2; ++jb)
+          for (int jb = 0; jb < 2; ++jb)
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
+            for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            *reinterpret_cast<_Float16*>(lds + (wa * 64 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) * LD +
-                                         2 * (wb * 64 + jb * 32 + (lane & 31))) = (_Float16)acc[ib][jb][r];
-      __syncthreads();
-      for (int i = threadIdx.x; i < kSmTile * 16; i += 256) {
-        const int row = i >> 4, k = (i & 15) * 8;
-        if (a0 + row < S.nx)
-          *reinterpret_cast<u32x4*>(static_cast<char*>(O.gt) + (a0 + row) * O.gt_row_bytes + (b0 + k) / PER * 128 + plane * 64 +
-                                    (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+              for (int r = 0; r < 16; ++r)
+                *reinterpret_cast<_Float16*>(lds + (ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) * LD +
+                                             2 * (wb * 64 + jb * 32 + (lane & 31))) = (_Float16)acc[ib][jb][r];
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 128 * 16; i += 256) {
+          const int row = i >> 4, k = (i & 15) * 8;
+          if (x0 + row < S.nx)
+            *reinterpret_cast<u32x4*>(static_cast<char*>(O.gt) + (x0 + row) * O.gt_row_bytes + (b0 + k) / PER * 64 + plane * 32 +
+                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+        }
+        __syncthreads();
       }
-      __syncthreads();
     }
     if (PLANES == 2 && plane == 0) {
 #pragma unroll
       for (int jb = 0; jb < 2; ++jb)
 #pragma unroll
-        for (int ib = 0; ib < 2; ++ib)
+        for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[ib][jb][r] -= (float)(_Float16)acc[ib][jb][r];
     }
   }
+}
+
+// Four elements at index i of an array of the vectors' type, the first n of them; whole: together (i a multiple of 4)
+template <typename T>
+__device__ __forceinline__ void store_4_as(T* p, int n, bool whole, const float (&v)[4]) {
+  if (whole) {
+    T e[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) e[u] = (T)v[u];
+    __builtin_memcpy(p, e, sizeof(e));
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (u < n) p[u] = (T)v[u];
+  }
+}
+__device__ __forceinline__ void store_4(void* p, int64_t i, int n, bool whole, int dtype, const float (&v)[4]) {
+  if (dtype == 0) store_4_as(static_cast<float*>(p) + i, n, whole, v);
+  else if (dtype == 1) store_4_as(static_cast<_Float16*>(p) + i, n, whole, v);
+  else store_4_as(static_cast<__bf16*>(p) + i, n, whole, v);
 }
 
 // ---- long products -------------------------------------------------------------------------
@@ -870,9 +924,11 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
 // next block from the last-level cache.  Fragments of the next 16 K elements are read while the present ones multiply.
 constexpr int kBigTile = 256;
 constexpr int kBigStage = 2 * kBigTile * 128;
-template <int PLANES>
+// With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type.
+template <int PLANES, bool DIRECT>
 __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix B, int64_t kblocks, int splits, int add,
-                                                            float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb) {
+                                                            float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb,
+                                                            const float* __restrict__ sa, float alpha, int dtype, int d) {
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   const int64_t tiles = ta * tb;
@@ -934,11 +990,11 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
         if (ks < 3) fragments(ks + 1, a[(ks + 1) & 1], b[(ks + 1) & 1]);
         products(a[ks & 1], b[ks & 1]);
       }
-    } else {                                          // heads 0, 1 and tails 2, 3: hi hi + hi lo + lo hi
+    } else {                                          // two units of heads and tails: hi hi + hi lo + lo hi
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        fragments(ks, a[0], b[0]);
-        fragments(ks + 2, a[1], b[1]);
+        fragments(2 * ks, a[0], b[0]);
+        fragments(2 * ks + 1, a[1], b[1]);
         products(a[0], b[0]);
         products(a[0], b[1]);
         products(a[1], b[0]);
@@ -950,6 +1006,20 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
   for (int jb = 0; jb < 2; ++jb) {
     const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
     if (b >= B.rows) continue;
+    if constexpr (DIRECT) {
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int a = (int)a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;
+          if (a >= d) continue;
+          float v[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] = a + u < d ? acc[ib][jb][r + u] * sa[a + u] * alpha : 0.f;
+          store_4(part, b * d + a, d - a, (d & 3) == 0, dtype, v);
+        }
+      continue;
+    }
     float* out = part + (split * B.rows + b) * ld;
 #pragma unroll
     for (int ib = 0; ib < 4; ++ib)
@@ -957,6 +1027,39 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
       for (int r = 0; r < 16; r += 4) {
         const int64_t a = a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;
         if (a >= ld) continue;                                      // (ld is a multiple of 4 and at least A.rows)
+        float4 v = make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
+        float4* o = reinterpret_cast<float4*>(out + a);
+        if (add) { const float4 w = *o; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
+        *o = v;
+      }
+  }
+}
+
+// The same on the tiles of the scores, for products that give 256 x 256 tiles too few workgroups.  K in units.
+template <int PLANES>
+__global__ __launch_bounds__(256, 2) void sm_product_small_kernel(SmMatrix A, SmMatrix B, int64_t kunits, int splits, int add,
+                                                                  float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb) {
+  extern __shared__ __align__(16) char lds[];
+  int64_t ia, ib_;
+  const int64_t tiles = ta * tb;
+  const int split = (int)(blockIdx.x / tiles);
+  tile_of(blockIdx.x - split * tiles, ta, tb, &ia, &ib_);
+  const int64_t a0 = ia * kTileA, b0 = ib_ * kTileB;
+  const int64_t k0 = kunits * split / splits, k1 = kunits * (split + 1) / splits;
+  f32x16 acc[4][2] = {};
+  if (k1 > k0) TileMul<PLANES, false>::run(A, a0, B, b0, k0, k1, lds, acc);
+  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+#pragma unroll
+  for (int jb = 0; jb < 2; ++jb) {
+    const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
+    if (b >= B.rows) continue;
+    float* out = part + (split * B.rows + b) * ld;
+#pragma unroll
+    for (int ib = 0; ib < 4; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int64_t a = a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;
+        if (a >= ld) continue;
         float4 v = make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
         float4* o = reinterpret_cast<float4*>(out + a);
         if (add) { const float4 w = *o; v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w; }
@@ -981,11 +1084,12 @@ __global__ __launch_bounds__(256) void sm_product_out_kernel(const float* __rest
   out[i] = (typename Elem<DT>::T)(v * alpha);
 }
 
-__global__ __launch_bounds__(256) void sm_sum_parts_kernel(const float* __restrict__ part, int64_t parts, int64_t ld,
+__global__ __launch_bounds__(64) void sm_sum_parts_kernel(const float* __restrict__ part, int64_t parts, int64_t ld,
                                                            int64_t n, float* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x;
   if (i >= n) return;
   float v = 0.f;
+#pragma unroll 8
   for (int64_t p = 0; p < parts; ++p) v += part[p * ld + i];
   out[i] = v;
 }
@@ -997,7 +1101,8 @@ __global__ __launch_bounds__(64) void sm_zero_bytes_kernel(unsigned char* __rest
   if ((int)threadIdx.x < n) p[threadIdx.x] = 0;
 }
 
-inline int64_t tiles(int64_t n) { return (n + kSmTile - 1) / kSmTile; }
+inline int64_t tiles_a(int64_t n) { return (n + kTileA - 1) / kTileA; }
+inline int64_t tiles_b(int64_t n) { return (n + kTileB - 1) / kTileB; }
 inline unsigned grid_of(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
 }  // namespace
@@ -1033,7 +1138,7 @@ void prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bi
   const unsigned gy = (unsigned)(n < 64 * 256 ? (n + 63) / 64 : 256);
   const int64_t per = (n + gy - 1) / gy;
   launch_sm_zero(colmax, (int64_t)d * 4, st);
-  sm_colmax_kernel<DT><<<dim3(grid_of(d, 64), gy), 256, 0, st>>>(static_cast<const T*>(x), n, d, bias, factor, per, colmax);
+  sm_colmax_kernel<DT><<<dim3(grid_of(d, 64 * 16 / (int)sizeof(T)), gy), 256, 0, st>>>(static_cast<const T*>(x), n, d, bias, factor, per, colmax);
   sm_prep_cols_kernel<DT, PLANES><<<dim3(grid_of(np, 64), grid_of(d, 64)), 256, 0, st>>>(
       static_cast<const T*>(x), n, d, np, bias, factor, colmax, static_cast<char*>(planes), scale);
 }
@@ -1048,7 +1153,7 @@ void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const
 }
 
 void launch_sm_scores(const SmForm& f, bool direct, const SmScores& s, const SmRecords& r, bool second, hipStream_t st) {
-  const int64_t ta = tiles(s.nx), tb = tiles(s.nq);
+  const int64_t ta = tiles_a(s.nx), tb = tiles_b(s.nq);
   const unsigned g = (unsigned)(ta * tb);
   auto run = [&](auto kern) { kern<<<g, 256, kTileLds, st>>>(s, r, ta, tb); };
   if (f.planes == 2) { if (second) run(sm_scores_kernel<2, false, true>); else run(sm_scores_kernel<2, false, false>); }
@@ -1098,23 +1203,57 @@ void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, flo
 }
 
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st) {
-  const int64_t ta = tiles(s.nx), tb = tiles(s.nq);
+  const int64_t ta = tiles_a(s.nx), tb = tiles_b(s.nq);
   const unsigned g = (unsigned)(ta * tb);
   if (f.planes == 2) sm_gradients_kernel<2, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
   else if (direct && f.dtype == 2) sm_gradients_kernel<1, true><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
   else sm_gradients_kernel<1, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
 }
 
-void launch_sm_product(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, int splits, bool add,
+// Splits of K that give a product some 256 workgroups, eight 128-byte blocks each at least; big: tiles of 256 x 256, where
+// they are a quarter of that or more by themselves (a smaller product waits for its few tiles: 96 x 1024 by 1024 took
+// 20.7 us on 16 big workgroups and 10.6 us on smaller tiles).
+SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
+  SmProductPlan p;
+  const int64_t big = (rows_a + kBigTile - 1) / kBigTile * ((rows_b + kBigTile - 1) / kBigTile);
+  p.big = big >= 48;
+  const int64_t n = p.big ? big : tiles_a(rows_a) * tiles_b(rows_b), most = kblocks / (p.big ? 8 : 4);
+  int64_t want = p.big ? (256 + n / 2) / n : (512 + n - 1) / n;
+  if (want > most) want = most;
+  if (want > 16) want = 16;
+  p.splits = want < 1 ? 1 : (int)want;
+  return p;
+}
+
+void launch_sm_product(const SmForm& f, const SmProductPlan& pp, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, bool add,
                        float* part, int64_t ld, hipStream_t st) {
+  if (pp.big) {
+    const int64_t ta = (A.rows + kBigTile - 1) / kBigTile, tb = (B.rows + kBigTile - 1) / kBigTile;
+    const unsigned g = (unsigned)(ta * tb * pp.splits);
+    auto run = [&](auto kern) {
+      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBigStage);
+      kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb, nullptr, 0.f, 0, 0);
+    };
+    if (f.planes == 2) run(sm_product_kernel<2, false>);
+    else run(sm_product_kernel<1, false>);
+  } else {
+    const int64_t ta = tiles_a(A.rows), tb = tiles_b(B.rows);
+    const unsigned g = (unsigned)(ta * tb * pp.splits);
+    if (f.planes == 2) sm_product_small_kernel<2><<<g, 256, kTileLds, st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
+    else sm_product_small_kernel<1><<<g, 256, kTileLds, st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
+  }
+}
+
+void launch_sm_product_direct(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, const float* sa,
+                              float alpha, int dtype, void* out, hipStream_t st) {
   const int64_t ta = (A.rows + kBigTile - 1) / kBigTile, tb = (B.rows + kBigTile - 1) / kBigTile;
-  const unsigned g = (unsigned)(ta * tb * splits);
+  const unsigned g = (unsigned)(ta * tb);
   auto run = [&](auto kern) {
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBigStage);
-    kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, splits, add ? 1 : 0, part, ld, ta, tb);
+    kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, 1, 0, static_cast<float*>(out), 0, ta, tb, sa, alpha, dtype, (int)A.rows);
   };
-  if (f.planes == 2) run(sm_product_kernel<2>);
-  else run(sm_product_kernel<1>);
+  if (f.planes == 2) run(sm_product_kernel<2, true>);
+  else run(sm_product_kernel<1, true>);
 }
 
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* sa, const float* sb,
@@ -1126,5 +1265,5 @@ void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t 
 }
 
 void launch_sm_sum_parts(const float* part, int64_t n_parts, int64_t ld, int64_t n, float* out, hipStream_t st) {
-  sm_sum_parts_kernel<<<grid_of(n, 256), 256, 0, st>>>(part, n_parts, ld, n, out);
+  sm_sum_parts_kernel<<<grid_of(n, 64), 64, 0, st>>>(part, n_parts, ld, n, out);
 }

@@ -7,16 +7,17 @@
 #include "store.hpp"
 
 // ---- log-probabilities over rows (kernels_logprob.hip) ---------------------------
-// A matrix as the matrix cores read it: rows of whole 128-byte K blocks, `rows` of them that exist.  A K block holds
-// 64 fp16 or bf16 elements, or (planes == 2) 32 fp16 heads and behind them their 32 fp16 tails.  scale: factor of every
-// row (a power of two), or null (ones).
+// A matrix as the matrix cores read it: rows of whole 128-byte K blocks (two units of 64 bytes), `rows` of them that
+// exist.  A K unit holds 32 fp16 or bf16 elements, or (planes == 2) 16 fp16 heads and behind them their 16 fp16 tails.
+// scale: factor of every row (a power of two), or null (ones).
 struct SmMatrix {
   const void* p = nullptr;
   int64_t row_bytes = 0;
   int64_t rows = 0;
   const float* scale = nullptr;
 };
-constexpr int kSmTile = 128;        // rows of either operand that a workgroup takes
+constexpr int kSmTileRows = 256;    // rows and queries that a workgroup takes
+constexpr int kSmTileQueries = 128;
 constexpr int kSmRecRows = 128;     // rows that a softmax record covers
 constexpr int kSmFewQueries = 64;   // up to here the rows are streamed past all queries
 
@@ -36,7 +37,7 @@ void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const
 
 struct SmScores {                   // s = scale <q, x> + bias for rows x0 .. x0 + nx of x
   SmMatrix x, q;
-  int64_t kblocks = 0;              // K blocks of a row
+  int64_t kunits = 0;               // K units of a row
   int64_t nx = 0, nq = 0;
   const float* bias = nullptr;      // of these rows
   float scale = 1.f;
@@ -44,7 +45,7 @@ struct SmScores {                   // s = scale <q, x> + bias for rows x0 .. x0
 struct SmRecords {                  // softmax of 128 rows: {max, sum, sum e (s - max), second best | position of the max}
   float4* rec = nullptr;            // [nq, parts]
   int64_t parts = 0;
-  float* keep = nullptr;            // [nq, keep_ld] the scores themselves, or null
+  float* keep = nullptr;            // [nq, keep_ld] the scores themselves, or null (keep_ld: whole tiles of rows)
   int64_t keep_ld = 0;
 };
 void launch_sm_scores(const SmForm& f, bool direct, const SmScores& s, const SmRecords& r, bool second, hipStream_t st);
@@ -71,9 +72,14 @@ struct SmGOut {
   float* db; int64_t db_ld;         // [query tiles, db_ld] partial column sums, or null
 };
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st);
-// out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over `splits` workgroups: part[split][b][ld]
-void launch_sm_product(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, int splits, bool add,
+// out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over workgroups: part[split][b][ld]
+struct SmProductPlan { bool big; int splits; };
+SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks);
+void launch_sm_product(const SmForm& f, const SmProductPlan& p, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, bool add,
                        float* part, int64_t ld, hipStream_t st);
+// out[b][a] = alpha scale_a[a] sum_k A[a][k] B[b][k], in `dtype`
+void launch_sm_product_direct(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, const float* scale_a,
+                              float alpha, int dtype, void* out, hipStream_t st);
 // out[b][a] = alpha scale_a[a] scale_b[b] sum_split part[split][b][a]
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* scale_a,
                            const float* scale_b, float alpha, int dtype, void* out, hipStream_t st);

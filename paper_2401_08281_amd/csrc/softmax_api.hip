@@ -56,13 +56,13 @@ LogprobPlan logprob_plan(int64_t nb, int64_t nq, int d, int dtype, int k) {
   p.few = nq <= kSmFewQueries;
   p.direct = rows_direct(dtype, d);
   p.parts = (nb + kSmRecRows - 1) / kSmRecRows;
-  p.keep_ld = p.parts * kSmRecRows;
+  p.keep_ld = round_up(nb, kSmTileRows);
   // A record that holds two of the k best costs its 128 scores again, some 30 ns of the device a query, and k^2 / (2 parts)
   // records do on average; a kept score costs 8 bytes of traffic, some 2 ps.  They break even near 8 records for each of
   // the k.
   p.keep = k > 0 && p.parts <= 8 * (int64_t)k;
   const int64_t per = p.parts * (int64_t)sizeof(float4) + (p.keep ? p.keep_ld * 4 : 0);
-  p.piece = std::min(nq, std::max<int64_t>(kSmTile, per > 0 ? kPieceBytes / per / kSmTile * kSmTile : nq));
+  p.piece = std::min(nq, std::max<int64_t>(kSmTileQueries, per > 0 ? kPieceBytes / per / kSmTileQueries * kSmTileQueries : nq));
   p.kblocks = p.f.blocks(d);
   p.row_bytes = p.direct ? d * elem_bytes(dtype) : p.kblocks * 128;
   Carver c;
@@ -82,15 +82,9 @@ struct GradPlan {
   SmForm f;
   bool direct;
   int64_t kblocks, row_bytes, chunk, ld, g_row, gt_row, xt_row, qt_row;
-  int splits_q, splits_x;
+  SmProductPlan to_q, to_x;
   int64_t o_x, o_xs, o_q, o_qs, o_xt, o_xts, o_qt, o_qts, o_cm, o_coef, o_bound, o_g, o_gt, o_dq, o_dx, o_db, bytes;
 };
-
-// Workgroups that a product should have: one a CU.  Fewer tiles than that share their K blocks out, 8 blocks each at least.
-int product_splits(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
-  const int64_t tiles = (rows_a + 255) / 256 * ((rows_b + 255) / 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({16, (256 + tiles / 2) / tiles, kblocks / 8}));
-}
 
 GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   GradPlan p{};
@@ -99,15 +93,15 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   p.kblocks = p.f.blocks(d);
   p.row_bytes = p.direct ? d * elem_bytes(dtype) : p.kblocks * 128;
   const int64_t el = 2 * p.f.planes;
-  const int64_t nqp = round_up(nq, kSmTile), nbp = round_up(nb, kSmTile);
-  p.chunk = std::min(nbp, std::max<int64_t>(kSmTile, kPieceBytes / (2 * el * nqp) / kSmTile * kSmTile));
+  const int64_t nqp = round_up(nq, kSmTileQueries), nbp = round_up(nb, kSmTileRows);
+  p.chunk = std::min(nbp, std::max<int64_t>(kSmTileRows, kPieceBytes / (2 * el * nqp) / kSmTileRows * kSmTileRows));
   p.ld = round_up(d, 4);
   p.g_row = p.chunk * el;
   p.gt_row = nqp * el;
   p.xt_row = p.f.blocks(nb) * 128;
   p.qt_row = p.f.blocks(nq) * 128;
-  p.splits_q = product_splits(d, nq, p.f.blocks(p.chunk));
-  p.splits_x = product_splits(d, p.chunk, p.f.blocks(nq));
+  p.to_q = plan_sm_product(d, nq, p.f.blocks(p.chunk));
+  p.to_x = plan_sm_product(d, p.chunk, p.f.blocks(nq));
   Carver c;
   if (!p.direct) {
     p.o_x = c.take(nb * p.row_bytes);
@@ -124,9 +118,9 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   p.o_bound = c.take(nq * 4);
   p.o_g = c.take(nq * p.g_row);
   p.o_gt = c.take(p.chunk * p.gt_row);
-  p.o_dq = c.take(p.splits_q * nq * p.ld * 4);
-  p.o_dx = c.take(p.splits_x * p.chunk * p.ld * 4);
-  p.o_db = c.take(nqp / kSmTile * p.chunk * 4);
+  p.o_dq = c.take(p.to_q.splits * nq * p.ld * 4);
+  p.o_dx = c.take(!p.to_x.big || p.to_x.splits > 1 ? p.to_x.splits * p.chunk * p.ld * 4 : 0);
+  p.o_db = c.take(nqp / kSmTileQueries * p.chunk * 4);
   p.bytes = c.off;
   return p;
 }
@@ -227,12 +221,12 @@ int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq, int32_
   if (misaligned(x, 16) || misaligned(q, 16)) return fail(VS_ERR_INVALID_ARG, "%s: x and q have to be 16-byte aligned", who);
   const LogprobPlan p = logprob_plan(nb, nq, d, dtype, k);
   if (int rc = check_space(who, workspace, workspace_bytes, p.bytes)) return rc;
-  if (p.parts * ((p.piece + kSmTile - 1) / kSmTile) >= (int64_t)1 << 31)
+  if (p.parts * ((p.piece + kSmTileQueries - 1) / kSmTileQueries) >= (int64_t)1 << 31)
     return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
   SmScores s;
-  s.kblocks = p.kblocks; s.nx = nb; s.bias = bias; s.scale = scale;
+  s.kunits = 2 * p.kblocks; s.nx = nb; s.bias = bias; s.scale = scale;
   s.x = SmMatrix{x, p.row_bytes, nb, nullptr};
   s.q = SmMatrix{q, p.row_bytes, nq, nullptr};
   if (!p.few && !p.direct && nb > 0) {
@@ -294,8 +288,8 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     return fail(VS_ERR_INVALID_ARG, "%s: x and q have to be 16-byte aligned, their gradients 4-byte", who);
   const GradPlan p = grad_plan(nb, nq, d, dtype);
   if (int rc = check_space(who, workspace, workspace_bytes, p.bytes)) return rc;
-  const int64_t tq = (nq + kSmTile - 1) / kSmTile;
-  if (tq * (p.chunk / kSmTile) >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  const int64_t tq = (nq + kSmTileQueries - 1) / kSmTileQueries;
+  if (tq * (p.chunk / kSmTileRows) >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
   if (!out_dq && !out_dx && !out_dbias) return VS_OK;
   char* ws = static_cast<char*>(workspace);
   auto at = [&](int64_t o) { return reinterpret_cast<float*>(ws + o); };
@@ -304,7 +298,7 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
   SmGrads g{lse, entropy, targets, nt, nt > 0 ? g_logp : nullptr, g_lse, g_entropy};
   launch_sm_coefs(g, nq, nb, reinterpret_cast<float4*>(ws + p.o_coef), bound, st);
   SmScores s;
-  s.kblocks = p.kblocks; s.nq = nq; s.scale = scale;
+  s.kunits = 2 * p.kblocks; s.nq = nq; s.scale = scale;
   const char* xp = static_cast<const char*>(x);
   const float* xs = nullptr;
   s.q = SmMatrix{q, p.row_bytes, nq, nullptr};
@@ -328,17 +322,21 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     launch_sm_gradients(p.f, p.direct, s, o, st);
     if (out_dq) {
       const SmMatrix a{ws + p.o_xt + x0 / p.f.per_block() * 128, p.xt_row, d, nullptr}, b{ws + p.o_g, p.g_row, nq, nullptr};
-      launch_sm_product(prod, a, b, p.f.blocks(n), p.splits_q, x0 > 0, at(p.o_dq), p.ld, st);
+      launch_sm_product(prod, p.to_q, a, b, p.f.blocks(n), x0 > 0, at(p.o_dq), p.ld, st);
     }
     if (out_dx) {
       const SmMatrix a{ws + p.o_qt, p.qt_row, d, nullptr}, b{ws + p.o_gt, p.gt_row, n, nullptr};
-      launch_sm_product(prod, a, b, p.f.blocks(nq), p.splits_x, false, at(p.o_dx), p.ld, st);
-      launch_sm_product_out(at(p.o_dx), p.splits_x, n, p.ld, d, at(p.o_qts), nullptr, alpha, dtype,
-                            static_cast<char*>(out_dx) + x0 * d * elem_bytes(dtype), st);
+      char* dx = static_cast<char*>(out_dx) + x0 * d * elem_bytes(dtype);
+      if (p.to_x.big && p.to_x.splits == 1) {
+        launch_sm_product_direct(prod, a, b, p.f.blocks(nq), at(p.o_qts), alpha, dtype, dx, st);
+      } else {
+        launch_sm_product(prod, p.to_x, a, b, p.f.blocks(nq), false, at(p.o_dx), p.ld, st);
+        launch_sm_product_out(at(p.o_dx), p.to_x.splits, n, p.ld, d, at(p.o_qts), nullptr, alpha, dtype, dx, st);
+      }
     }
     if (out_dbias) launch_sm_sum_parts(at(p.o_db), tq, p.chunk, n, out_dbias + x0, st);
   }
-  if (out_dq) launch_sm_product_out(at(p.o_dq), p.splits_q, nq, p.ld, d, at(p.o_xts), bound, alpha, dtype, out_dq, st);
+  if (out_dq) launch_sm_product_out(at(p.o_dq), p.to_q.splits, nq, p.ld, d, at(p.o_xts), bound, alpha, dtype, out_dq, st);
   return launched(who);
 }
 
