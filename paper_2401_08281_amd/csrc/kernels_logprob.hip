@@ -466,14 +466,15 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// <q, x_j> for eight rows at once, eight lanes a row; every lane of a row's group gets the sum
-template <typename T>
-__device__ __forceinline__ float dot_8_rows(const T* __restrict__ q, const T* __restrict__ row, int d) {
+// <q, x_j> for eight rows at once, eight lanes a row; every lane of a row's group gets the sum.  LANES = 64: one row.
+template <int LANES, typename T>
+__device__ __forceinline__ float dot_rows(const T* __restrict__ q, const T* __restrict__ row, int d) {
   constexpr int V = 16 / sizeof(T);
-  const int l = lane_id() & 7;
+  const int l = lane_id() & (LANES - 1);
   float acc = 0.f;
   int k = l * V;
-  for (; k + V <= d; k += 8 * V) {
+#pragma unroll 4
+  for (; k + V <= d; k += LANES * V) {
     T a[V], b[V];
     __builtin_memcpy(a, q + k, 16);
     __builtin_memcpy(b, row + k, 16);
@@ -481,17 +482,64 @@ __device__ __forceinline__ float dot_8_rows(const T* __restrict__ q, const T* __
     for (int i = 0; i < V; ++i) acc = __builtin_fmaf(to_f32(a[i]), to_f32(b[i]), acc);
   }
   for (int i = k; i < d && i < k + V; ++i) acc = __builtin_fmaf(to_f32(q[i]), to_f32(row[i]), acc);
-  acc += __shfl_xor(acc, 1);
-  acc += __shfl_xor(acc, 2);
-  acc += __shfl_xor(acc, 4);
+#pragma unroll
+  for (int w = 1; w < LANES; w <<= 1) acc += __shfl_xor(acc, w);
   return acc;
+}
+
+// Maximum over the wavefront in every lane: inside rows of 16 lanes by DPP, across them by two broadcasts.
+__device__ __forceinline__ float wave_max_dpp(float v) {
+  auto step = [&](int o) { v = fmaxf(v, __int_as_float(o)); };
+  const int lo = __float_as_int(neg_inf());
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x111, 0xF, 0xF, false));   // row_shr 1, 2, 4, 8
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x112, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x114, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x118, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x142, 0xA, 0xF, false));   // row_bcast 15, 31
+  step(__builtin_amdgcn_update_dpp(lo, __float_as_int(v), 0x143, 0xC, 0xF, false));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+constexpr int kTakeBest = 16, kTakePer = 8;
+// The k best of the wavefront's records (thread's i-th: threadIdx.x + 256 i) as ascending keys of {maximum, record}: the
+// best of the lanes' bests k times, its lane going through its own again.
+__device__ __forceinline__ void wave_take_best(const float4 (&rec)[kTakePer], int k, u64* out) {
+  u32 gone = 0;                                           // which of this lane's are taken
+  float best;
+  int at;
+  auto mine = [&]() {
+    best = neg_inf();
+    at = 0;
+#pragma unroll
+    for (int i = 0; i < kTakePer; ++i)
+      if (rec[i].x > best && !((gone >> i) & 1u)) { best = rec[i].x; at = i; }
+  };
+  mine();
+  for (int r = 0; r < k; ++r) {
+    const float top = wave_max_dpp(best);
+    u64 key = KEY_EMPTY;
+    if (top > neg_inf()) {
+      const u32 id = threadIdx.x + 256u * (u32)at;
+      u64 have = __ballot(best == top);
+      u32 win = __builtin_amdgcn_readlane((int)id, __ffsll(have) - 1);
+      for (have &= have - 1; have; have &= have - 1) {    // equal maxima: the smaller record
+        const u32 o = __builtin_amdgcn_readlane((int)id, __ffsll(have) - 1);
+        win = o < win ? o : win;
+      }
+      key = make_key(top, win, 1);
+      if (best == top && id == win) { gone |= 1u << at; mine(); }
+    }
+    if (lane_id() == 0) out[r] = key;
+  }
 }
 
 // One workgroup per query.  The k best rows lie in the k records with the best maxima (a row outside them is beaten by k
 // maxima; records cover consecutive rows, so ties fall to the smaller row as well).  Of such a record only the maximum
 // can count unless its second best reaches the k-th best maximum: then its 128 scores are computed again in fp32.
 // Where that would be common (few records, or many alternatives) the scores have been kept, and are read instead.
-template <int DT>
+// TAKE: up to kTakeBest alternatives of up to 256 kTakePer records (262,144 rows), which stay in registers and are picked
+// one by one; more go through the reservoir selection, whose first sort alone takes some 700 instructions.
+template <int DT, bool TAKE>
 __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R) {
   typedef typename Elem<DT>::T T;
   constexpr int TOT = 128;
@@ -502,21 +550,48 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
   const int64_t qi = blockIdx.x;
   const int lane = lane_id(), wave = threadIdx.x >> 6;
   const float4* rec = R.rec + qi * R.parts;
+  const T* x = static_cast<const T*>(F.x);
+  const T* q = static_cast<const T*>(F.q) + qi * F.d;
+  const int64_t target = wave < F.nt ? F.targets[qi * F.nt + wave] : -1;
+  const bool target_in = target >= 0 && target < F.nb;
   float m = neg_inf();
-  for (int64_t p = threadIdx.x; p < R.parts; p += 256) m = fmaxf(m, rec[p].x);
-  m = wave_max(m);
+  float4 own[TAKE ? kTakePer : 1];
+  if (TAKE) {
+#pragma unroll
+    for (int i = 0; i < kTakePer; ++i) {
+      const int64_t p = threadIdx.x + 256 * i;
+      own[i] = p < R.parts ? rec[p] : make_float4(neg_inf(), 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < kTakePer; ++i) m = fmaxf(m, own[i].x);
+  } else {
+#pragma unroll 4
+    for (int64_t p = threadIdx.x; p < R.parts; p += 256) m = fmaxf(m, rec[p].x);
+  }
+  // (of target `wave`, while the records are on their way)
+  const float target_score = wave < F.nt && F.nb > 0 ? dot_rows<64>(q, x + (target_in ? target : 0) * F.d, F.d) : 0.f;
+  m = wave_max_dpp(m);
   if (lane == 0) red[0][wave] = m;
   if (threadIdx.x == 0) shared_bound = KEY_EMPTY;
   __syncthreads();
   m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   float l = 0.f, h = 0.f;
-  for (int64_t p = threadIdx.x; p < R.parts; p += 256) {
-    const float4 r = rec[p];
-    softmax_join(m, r.x, r.y, r.z, &l, &h);
+  if (TAKE) {
+#pragma unroll
+    for (int i = 0; i < kTakePer; ++i) softmax_join(m, own[i].x, own[i].y, own[i].z, &l, &h);
+  } else {
+#pragma unroll 4
+    for (int64_t p = threadIdx.x; p < R.parts; p += 256) {
+      const float4 r = rec[p];
+      softmax_join(m, r.x, r.y, r.z, &l, &h);
+    }
   }
   l = wave_sum(l);
   h = wave_sum(h);
   if (lane == 0) { red[1][wave] = l; red[2][wave] = h; }
+  if constexpr (TAKE) {
+    if (F.k > 0) wave_take_best(own, F.k, slots + wave * TOT);
+  }
   __syncthreads();
   l = red[1][0] + red[1][1] + red[1][2] + red[1][3];
   h = red[2][0] + red[2][1] + red[2][2] + red[2][3];
@@ -526,17 +601,12 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
     F.lse[qi] = lse;
     F.entropy[qi] = empty ? 0.f : logl - h / l;
   }
-  const T* x = static_cast<const T*>(F.x);
-  const T* q = static_cast<const T*>(F.q) + qi * F.d;
-  const int group = lane >> 3;
-  for (int t0 = wave * 8; t0 < F.nt; t0 += 32) {
-    const int t = t0 + group;
-    const int64_t j = t < F.nt ? F.targets[qi * F.nt + t] : -1;
+  for (int t = wave; t < F.nt; t += 4) {
+    const int64_t j = t < 4 ? target : F.targets[qi * F.nt + t];
     const bool in = j >= 0 && j < F.nb;
     const float b = in && F.bias ? F.bias[j] : 0.f;
-    const float s = dot_8_rows(q, x + (in ? j : 0) * F.d, F.nb > 0 ? F.d : 0) * F.scale + b;
-    if ((lane & 7) == 0 && t < F.nt)
-      F.logp[qi * F.nt + t] = !in ? 0.f : (b == neg_inf() ? neg_inf() : s - lse);
+    const float dot = t < 4 || F.nb == 0 ? target_score : dot_rows<64>(q, x + (in ? j : 0) * F.d, F.d);
+    if (lane == 0) F.logp[qi * F.nt + t] = !in ? 0.f : (b == neg_inf() ? neg_inf() : dot * F.scale + b - lse);
   }
   if (F.k == 0) return;
   WaveSelect<2> sel;
@@ -544,6 +614,9 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
     sel.init(slots + wave * TOT, TOT, F.k, &shared_bound);
     sel.set_metric(1);
   };
+  const KeySink to{chosen, nullptr, nullptr, nullptr, nullptr, 1};
+  const int group = lane >> 3;
+  bool done = false;
   if (R.keep) {
     start();
     const float* s = R.keep + qi * R.keep_ld;
@@ -553,47 +626,63 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
       sel.push_value(v > neg_inf(), v, (u32)j);
     }
   } else {
-    start();
-    for (int64_t p0 = wave * 64; p0 < R.parts; p0 += 256) {
-      const int64_t p = p0 + lane;
-      const float v = p < R.parts ? rec[p].x : neg_inf();
-      sel.push_value(v > neg_inf(), v, (u32)p);
+    if (!TAKE) {
+      start();
+      for (int64_t p0 = wave * 64; p0 < R.parts; p0 += 256) {
+        const int64_t p = p0 + lane;
+        const float v = p < R.parts ? rec[p].x : neg_inf();
+        sel.push_value(v > neg_inf(), v, (u32)p);
+      }
+      sel.finish();
+      __syncthreads();
     }
-    sel.finish();
-    __syncthreads();
-    KeySink to{chosen, nullptr, nullptr, nullptr, nullptr, 1};
-    block_rank_merge(slots, TOT, 4, F.k, to, 0);
+    if (TAKE) {                                             // 4 k <= 64 keys, one a lane, to their places
+      if (wave == 0) {
+        const u64 mine = lane < 4 * F.k ? slots[lane / F.k * TOT + lane % F.k] : KEY_EMPTY;
+        int rank = 0;
+        for (int i = 0; i < 4 * F.k; ++i) {
+          const u64 o = __shfl(mine, i);
+          rank += o < mine || (o == mine && i < lane) ? 1 : 0;
+        }
+        if (lane < 4 * F.k && rank < F.k) chosen[rank] = mine;
+      }
+    } else {
+      block_rank_merge(slots, TOT, 4, F.k, to, 0);
+    }
     if (threadIdx.x == 0) shared_bound = KEY_EMPTY;
     __syncthreads();
-    const u64 last = chosen[F.k - 1];
+    // (VS_MAX_TOP = 64: one lane holds each of the chosen records)
+    const u64 last = chosen[F.k - 1], key = lane < F.k ? chosen[lane] : KEY_EMPTY;
     const float tau = last == KEY_EMPTY ? neg_inf() : key_value(last, 1);
-    start();
-    for (int c0 = 0; c0 < F.k; c0 += 64) {
-      const int c = c0 + lane;
-      const u64 key = c < F.k ? chosen[c] : KEY_EMPTY;
-      const u32 p = key_index(key);
-      const float w = key != KEY_EMPTY ? rec[p].w : 0.f;
-      const bool whole = key != KEY_EMPTY && w >= tau;
-      if (wave == 0) {                                      // the maximum alone
-        const u32 j = p * kSmRecRows + (__float_as_uint(w) & 127u);
-        sel.push(key != KEY_EMPTY && !whole, make_key(key_value(key, 1), j, 1));
-      }
-      for (u64 todo = __ballot(whole); todo; todo &= todo - 1) {
-        const u32 pw = __shfl(p, __ffsll(todo) - 1);
+    const u32 p = key_index(key);
+    const float w = key != KEY_EMPTY ? rec[p].w : 0.f;
+    const bool whole = key != KEY_EMPTY && w >= tau;
+    const u64 alone = make_key(key_value(key, 1), p * kSmRecRows + (__float_as_uint(w) & 127u), 1);
+    const u64 todo = __ballot(whole);
+    __syncthreads();                                        // (everybody has read what was chosen)
+    if (todo == 0) {                                        // the maxima are the best rows, in this order
+      if (wave == 0 && lane < F.k) chosen[lane] = key == KEY_EMPTY ? KEY_EMPTY : alone;
+      done = true;
+    } else {
+      start();
+      if (wave == 0) sel.push(key != KEY_EMPTY && !whole, alone);
+      for (u64 rest = todo; rest; rest &= rest - 1) {
+        const u32 pw = __shfl(p, __ffsll(rest) - 1);
         for (int r0 = wave * 8; r0 < kSmRecRows; r0 += 32) {
           const int64_t j = (int64_t)pw * kSmRecRows + r0 + group;
           const bool in = j < F.nb;
           const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
-          const float s = dot_8_rows(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b;
+          const float s = dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b;
           sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
         }
       }
     }
   }
-  sel.finish();
-  __syncthreads();
-  KeySink to{chosen, nullptr, nullptr, nullptr, nullptr, 1};
-  block_rank_merge(slots, TOT, 4, F.k, to, 0);
+  if (!done) {
+    sel.finish();
+    __syncthreads();
+    block_rank_merge(slots, TOT, 4, F.k, to, 0);
+  }
   __syncthreads();
   if ((int)threadIdx.x < F.k) {
     const u64 key = chosen[threadIdx.x];
@@ -611,39 +700,6 @@ __device__ __forceinline__ void row_scale(float mx, float* up, float* down) {
   *up = __builtin_ldexpf(1.f, e);
   *down = __builtin_ldexpf(1.f, -e);
 }
-// element v (scaled) at position k of a row of K blocks
-template <int PLANES>
-__device__ __forceinline__ void put_planes(char* row, int64_t k, float v) {
-  const _Float16 hi = (_Float16)v;
-  if (PLANES == 1) {
-    reinterpret_cast<_Float16*>(row)[k] = hi;
-  } else {
-    _Float16* b = reinterpret_cast<_Float16*>(row + (k >> 4) * 64) + (k & 15);
-    b[0] = hi;
-    b[16] = (_Float16)(v - (float)hi);
-  }
-}
-
-template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
-                                                           int64_t dp, const float* __restrict__ bias,
-                                                           char* __restrict__ planes, float* __restrict__ scale) {
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= n) return;
-  const int lane = lane_id();
-  const typename Elem<DT>::T* row = x + r * d;
-  const bool gone = bias && bias[r] == neg_inf();
-  float mx = 0.f;
-  if (!gone)
-    for (int k = lane; k < d; k += 64) mx = fmaxf(mx, fabsf(to_f32(row[k])));
-  mx = wave_max(mx);
-  float up, down;
-  row_scale(mx, &up, &down);
-  char* out = planes + r * (dp * 2 * PLANES);
-  for (int k = lane; k < dp; k += 64) put_planes<PLANES>(out, k, k < d && !gone ? to_f32(row[k]) * up : 0.f);
-  if (lane == 0) scale[r] = down;
-}
-
 // Elements k .. k + 15 / sizeof(T) of a row as floats, zeros past its end (vec: rows of whole 16-byte pieces)
 template <typename T>
 __device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int d, bool vec, float (&v)[16 / sizeof(T)]) {
@@ -657,6 +713,74 @@ __device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = k + i < d ? to_f32(row[k + i]) : 0.f;
   }
+}
+
+// 16 lanes a row, 16 bytes a lane and step; rows of up to kPrepSteps steps are read once and stay in registers.
+constexpr int kPrepSteps = 8;
+template <int DT, int PLANES>
+__global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
+                                                           int64_t dp, const float* __restrict__ bias,
+                                                           char* __restrict__ planes, float* __restrict__ scale) {
+  typedef typename Elem<DT>::T T;
+  constexpr int V = 16 / sizeof(T);
+  const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (r >= n) return;                                                // (whole groups of 16 lanes)
+  const int l = threadIdx.x & 15;
+  const bool vec = d % V == 0, gone = bias && bias[r] == neg_inf(), kept = dp <= 16 * V * kPrepSteps;
+  const T* row = x + r * d;
+  float v[kPrepSteps][V];
+  float mx = 0.f;
+  if (kept) {
+#pragma unroll
+    for (int i = 0; i < kPrepSteps; ++i) {
+      const int k = (i * 16 + l) * V;
+#pragma unroll
+      for (int u = 0; u < V; ++u) v[i][u] = 0.f;
+      if (!gone && k < d) load_piece(row, k, d, vec, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPrepSteps; ++i)
+#pragma unroll
+      for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[i][u]));
+  } else if (!gone) {
+    for (int k = l * V; k < d; k += 16 * V) {
+      load_piece(row, k, d, vec, v[0]);
+#pragma unroll
+      for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[0][u]));
+    }
+  }
+#pragma unroll
+  for (int w = 1; w < 16; w <<= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
+  float up, down;
+  row_scale(mx, &up, &down);
+  char* out = planes + r * (dp * 2 * PLANES);
+  auto put = [&](int64_t k, const float (&e)[V]) {
+    _Float16 hi[V], lo[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      const float t = e[u] * up;
+      hi[u] = (_Float16)t;
+      lo[u] = (_Float16)(t - (float)hi[u]);
+    }
+    char* to = PLANES == 1 ? out + k * 2 : out + (k >> 4) * 64 + (k & 15) * 2;
+    __builtin_memcpy(to, hi, sizeof(hi));
+    if (PLANES == 2) __builtin_memcpy(to + 32, lo, sizeof(lo));
+  };
+  if (kept) {
+#pragma unroll
+    for (int i = 0; i < kPrepSteps; ++i) {
+      const int64_t k = (i * 16 + l) * V;
+      if (k < dp) put(k, v[i]);
+    }
+  } else {
+    for (int64_t k = l * V; k < dp; k += 16 * V) {
+#pragma unroll
+      for (int u = 0; u < V; ++u) v[0][u] = 0.f;
+      if (!gone && k < d) load_piece(row, (int)k, d, vec, v[0]);
+      put(k, v[0]);
+    }
+  }
+  if (l == 0) scale[r] = down;
 }
 
 // Largest size in every column: a thread goes down 16 bytes of columns.  (A maximum does not depend on the order, and
@@ -1120,7 +1244,7 @@ void launch_sm_prep_rows(const SmForm& f, const void* x, int64_t n, int d, const
                          hipStream_t st) {
   if (n == 0) return;
   const int64_t dp = f.blocks(d) * f.per_block();
-  const unsigned g = grid_of(n, 4);
+  const unsigned g = grid_of(n, 16);
   if (f.dtype == 0)
     sm_prep_rows_kernel<0, 2><<<g, 256, 0, st>>>(static_cast<const float*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
   else if (f.dtype == 1)
@@ -1193,9 +1317,14 @@ void launch_sm_scores_few(int dtype, const void* x, int64_t nb, const void* q, i
 
 void launch_sm_finish(const SmFinish& f, const SmRecords& r, hipStream_t st) {
   const unsigned g = (unsigned)f.nq;
-  if (f.dtype == 0) sm_finish_kernel<0><<<g, 256, 0, st>>>(f, r);
-  else if (f.dtype == 1) sm_finish_kernel<1><<<g, 256, 0, st>>>(f, r);
-  else sm_finish_kernel<2><<<g, 256, 0, st>>>(f, r);
+  const bool take = f.k <= kTakeBest && r.parts <= 256 * kTakePer && !r.keep;
+  auto run = [&](auto some, auto all) {
+    if (take) some<<<g, 256, 0, st>>>(f, r);
+    else all<<<g, 256, 0, st>>>(f, r);
+  };
+  if (f.dtype == 0) run(sm_finish_kernel<0, true>, sm_finish_kernel<0, false>);
+  else if (f.dtype == 1) run(sm_finish_kernel<1, true>, sm_finish_kernel<1, false>);
+  else run(sm_finish_kernel<2, true>, sm_finish_kernel<2, false>);
 }
 
 void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, hipStream_t st) {
