@@ -63,77 +63,79 @@ __device__ __forceinline__ void settle_products() {
 // pieces are stored at piece ^ ((row >> 2) & 3): a fragment read (32 rows x 2 pieces) then touches every bank evenly.
 // With two planes a unit holds 16 heads and their 16 tails, and one stage feeds hi*hi + hi*lo + lo*hi.
 // Against tiles of 128 x 128 by 64 x 64 (K units of 128 bytes), scores of 4096 x 65,536 x 768: measured beside the kernel.
+// Products and gradients of few tiles take 128 x 64 by 64 x 32 instead (IB, JB: 32-row and 32-query blocks of a wavefront).
 constexpr int kTileA = 256, kTileB = 128;
-constexpr int kStage = (kTileA + kTileB) * 64;
-constexpr int kTileLds = 2 * kStage;
+template <int IB, int JB>
+constexpr int tile_lds() { return 2 * 64 * (IB + JB) * 64; }
 
-template <int PLANES, bool BF16>
+template <int PLANES, bool BF16, int IB = 4, int JB = 2>
 struct TileMul {
+  static constexpr int TA = 64 * IB, TB = 64 * JB, kStage = (TA + TB) * 64;
   static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
     if constexpr (BF16)
       return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     else
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
-  // acc[ib][jb] of this wavefront: rows 128 wa + 32 ib .., queries 64 wb + 32 jb ..; K units [ku0, ku1), at least one
+  // acc[ib][jb] of this wavefront: rows 32 (IB wa + ib) .., queries 32 (JB wb + jb) ..; K units [ku0, ku1), at least one
   static __device__ __forceinline__ void run(const SmMatrix& A, int64_t a0, const SmMatrix& B, int64_t b0, int64_t ku0,
-                                             int64_t ku1, char* lds, f32x16 (&acc)[4][2]) {
+                                             int64_t ku1, char* lds, f32x16 (&acc)[IB][JB]) {
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     const int wa = wave & 1, wb = wave >> 1;
     // rows past the last one repeat it: their results are dropped
     const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
     const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
-    const int ra_max = (int)(A.rows - 1 - a0 < kTileA ? A.rows - 1 - a0 : kTileA - 1);
-    const int rb_max = (int)(B.rows - 1 - b0 < kTileB ? B.rows - 1 - b0 : kTileB - 1);
-    const char* ga[4];
-    const char* gb[2];
+    const int ra_max = (int)(A.rows - 1 - a0 < TA ? A.rows - 1 - a0 : TA - 1);
+    const int rb_max = (int)(B.rows - 1 - b0 < TB ? B.rows - 1 - b0 : TB - 1);
+    const char* ga[IB];
+    const char* gb[JB];
     const int piece = (lane & 3) ^ ((lane >> 4) & 3);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = (wave * 4 + i) * 16 + (lane >> 2);
+    for (int i = 0; i < IB; ++i) {
+      const int r = (wave * IB + i) * 16 + (lane >> 2);
       ga[i] = pa + (int64_t)(r < ra_max ? r : ra_max) * A.row_bytes + ku0 * 64 + piece * 16;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = (wave * 2 + i) * 16 + (lane >> 2);
+    for (int i = 0; i < JB; ++i) {
+      const int r = (wave * JB + i) * 16 + (lane >> 2);
       gb[i] = pb + (int64_t)(r < rb_max ? r : rb_max) * B.row_bytes + ku0 * 64 + piece * 16;
     }
     auto request = [&](int stage) {
       char* to = lds + stage * kStage;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < IB; ++i) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ga[i],
-                                         (__attribute__((address_space(3))) void*)(to + (wave * 4 + i) * 1024), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(to + (wave * IB + i) * 1024), 16, 0, 0);
         ga[i] += 64;
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < JB; ++i) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)gb[i],
-                                         (__attribute__((address_space(3))) void*)(to + kTileA * 64 + (wave * 2 + i) * 1024), 16, 0, 0);
+                                         (__attribute__((address_space(3))) void*)(to + TA * 64 + (wave * JB + i) * 1024), 16, 0, 0);
         gb[i] += 64;
       }
     };
-    const int ra = (wa * 128 + (lane & 31)) * 64, rb = kTileA * 64 + (wb * 64 + (lane & 31)) * 64, half = lane >> 5, sw = (lane >> 2) & 3;
+    const int ra = (wa * 32 * IB + (lane & 31)) * 64, rb = TA * 64 + (wb * 32 * JB + (lane & 31)) * 64, half = lane >> 5, sw = (lane >> 2) & 3;
     request(0);
     const int n = (int)(ku1 - ku0);
     for (int t = 0; t < n; ++t) {
       __syncthreads();                                  // the stage has landed, the other one is free
       const char* s = lds + (t & 1) * kStage;
-      u32x4 a[2][4], b[2][2];
+      u32x4 a[2][IB], b[2][JB];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const int off = ((2 * ks + half) ^ sw) * 16;
 #pragma unroll
-        for (int ib = 0; ib < 4; ++ib) a[ks][ib] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 64 + off);
+        for (int ib = 0; ib < IB; ++ib) a[ks][ib] = *reinterpret_cast<const u32x4*>(s + ra + ib * 32 * 64 + off);
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb) b[ks][jb] = *reinterpret_cast<const u32x4*>(s + rb + jb * 32 * 64 + off);
+        for (int jb = 0; jb < JB; ++jb) b[ks][jb] = *reinterpret_cast<const u32x4*>(s + rb + jb * 32 * 64 + off);
       }
       if (t + 1 < n) request((t + 1) & 1);
-      auto products = [&](const u32x4 (&fa)[4], const u32x4 (&fb)[2]) {
+      auto products = [&](const u32x4 (&fa)[IB], const u32x4 (&fb)[JB]) {
 #pragma unroll
-        for (int ib = 0; ib < 4; ++ib)
+        for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
-          for (int jb = 0; jb < 2; ++jb) acc[ib][jb] = mul(fa[ib], fb[jb], acc[ib][jb]);
+          for (int jb = 0; jb < JB; ++jb) acc[ib][jb] = mul(fa[ib], fb[jb], acc[ib][jb]);
       };
       products(a[0], b[0]);
       if constexpr (PLANES == 1) {
@@ -189,32 +191,33 @@ __device__ __forceinline__ Best join_mixed(Best a, Best b) {
 // The scores of a wavefront's tile in place of its products: s = acc * (row factor * query factor) + bias, -inf for
 // rows that do not exist (past the end, or bias -inf: whatever their products are).
 // rowdata: LDS, {row factor, bias} of the workgroup's 256 rows, filled here.
-__device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[4][2]) {
+template <int IB, int JB>
+__device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[IB][JB]) {
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1;
-  const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + kTileA <= S.nx;   // (the same in the workgroup)
+  const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + 64 * IB <= S.nx;   // (the same in the workgroup)
   if (!plain) {
     const int64_t j = a0 + threadIdx.x;
     const bool in = j < S.nx;
-    rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
+    if (threadIdx.x < 64 * IB) rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
     __syncthreads();
   }
-  float cq[2];
+  float cq[JB];
 #pragma unroll
-  for (int jb = 0; jb < 2; ++jb) {
-    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
     cq[jb] = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] : 1.f);
   }
 #pragma unroll
-  for (int ib = 0; ib < 4; ++ib)
+  for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       if (plain) {
-        acc[ib][0][r] *= cq[0];
-        acc[ib][1][r] *= cq[1];
-      } else {
-        const float2 rd = rowdata[wa * 128 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)];
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb) {
+        for (int jb = 0; jb < JB; ++jb) acc[ib][jb][r] *= cq[jb];
+      } else {
+        const float2 rd = rowdata[(wa * IB + ib) * 32 + (r & 3) + 8 * (r >> 2) + 4 * (lane >> 5)];
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) {
           const float s = acc[ib][jb][r] * rd.x * cq[jb] + rd.y;
           acc[ib][jb][r] = rd.y == neg_inf() ? neg_inf() : s;
         }
@@ -700,11 +703,11 @@ __device__ __forceinline__ void row_scale(float mx, float* up, float* down) {
   *up = __builtin_ldexpf(1.f, e);
   *down = __builtin_ldexpf(1.f, -e);
 }
-// Elements k .. k + 15 / sizeof(T) of a row as floats, zeros past its end (vec: rows of whole 16-byte pieces)
+// Elements k .. k + 15 / sizeof(T) of a row as floats, zeros past its end (one load wherever the row begins)
 template <typename T>
-__device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int d, bool vec, float (&v)[16 / sizeof(T)]) {
+__device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int d, float (&v)[16 / sizeof(T)]) {
   constexpr int V = 16 / sizeof(T);
-  if (vec && k < d) {
+  if (k + V <= d) {
     T e[V];
     __builtin_memcpy(e, row + k, 16);
 #pragma unroll
@@ -718,15 +721,18 @@ __device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int
 // 16 lanes a row, 16 bytes a lane and step; rows of up to kPrepSteps steps are read once and stay in registers.
 constexpr int kPrepSteps = 8;
 template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
-                                                           int64_t dp, const float* __restrict__ bias,
-                                                           char* __restrict__ planes, float* __restrict__ scale) {
+__global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d, int64_t dp) {
   typedef typename Elem<DT>::T T;
   constexpr int V = 16 / sizeof(T);
-  const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (r >= n) return;                                                // (whole groups of 16 lanes)
+  const SmSide& S = blockIdx.x < blocks0 ? side0 : side1;
+  const T* __restrict__ x = static_cast<const T*>(S.x);
+  const float* __restrict__ bias = S.bias;
+  char* __restrict__ planes = static_cast<char*>(S.rows);
+  float* __restrict__ scale = S.row_scale;
+  const int64_t r = (int64_t)(blockIdx.x < blocks0 ? blockIdx.x : blockIdx.x - blocks0) * 16 + (threadIdx.x >> 4);
+  if (r >= S.n) return;                                                // (whole groups of 16 lanes)
   const int l = threadIdx.x & 15;
-  const bool vec = d % V == 0, gone = bias && bias[r] == neg_inf(), kept = dp <= 16 * V * kPrepSteps;
+  const bool gone = bias && bias[r] == neg_inf(), kept = dp <= 16 * V * kPrepSteps;
   const T* row = x + r * d;
   float v[kPrepSteps][V];
   float mx = 0.f;
@@ -736,7 +742,7 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<D
       const int k = (i * 16 + l) * V;
 #pragma unroll
       for (int u = 0; u < V; ++u) v[i][u] = 0.f;
-      if (!gone && k < d) load_piece(row, k, d, vec, v[i]);
+      if (!gone && k < d) load_piece(row, k, d, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < kPrepSteps; ++i)
@@ -744,7 +750,7 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<D
       for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[i][u]));
   } else if (!gone) {
     for (int k = l * V; k < d; k += 16 * V) {
-      load_piece(row, k, d, vec, v[0]);
+      load_piece(row, k, d, v[0]);
 #pragma unroll
       for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[0][u]));
     }
@@ -776,7 +782,7 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<D
     for (int64_t k = l * V; k < dp; k += 16 * V) {
 #pragma unroll
       for (int u = 0; u < V; ++u) v[0][u] = 0.f;
-      if (!gone && k < d) load_piece(row, (int)k, d, vec, v[0]);
+      if (!gone && k < d) load_piece(row, (int)k, d, v[0]);
       put(k, v[0]);
     }
   }
@@ -786,22 +792,26 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(const typename Elem<D
 // Largest size in every column: a thread goes down 16 bytes of columns.  (A maximum does not depend on the order, and
 // non-negative floats are ordered as their bits.)
 template <int DT>
-__global__ __launch_bounds__(256) void sm_colmax_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
-                                                        const float* __restrict__ bias, const float* __restrict__ factor,
-                                                        int64_t rows_per, u32* __restrict__ colmax) {
+__global__ __launch_bounds__(256) void sm_colmax_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d, int64_t rows_per) {
   typedef typename Elem<DT>::T T;
   constexpr int V = 16 / sizeof(T);
+  const SmSide& S = blockIdx.y < blocks0 ? side0 : side1;
+  const T* __restrict__ x = static_cast<const T*>(S.x);
+  const float* __restrict__ bias = S.bias;
+  const float* __restrict__ factor = S.factor;
+  u32* __restrict__ colmax = S.colmax;
+  const int64_t n = S.n;
   __shared__ float part[4][64 * V];
   const int lane = lane_id(), wave = threadIdx.x >> 6, t = (blockIdx.x * 64 + lane) * V;
-  const bool vec = d % V == 0;
-  const int64_t r0 = (int64_t)blockIdx.y * rows_per, r1 = r0 + rows_per < n ? r0 + rows_per : n;
+  const int64_t r0 = (int64_t)(blockIdx.y < blocks0 ? blockIdx.y : blockIdx.y - blocks0) * rows_per;
+  const int64_t r1 = r0 + rows_per < n ? r0 + rows_per : n;
   float mx[V] = {};
   if (t < d)
 #pragma unroll 4
     for (int64_t r = r0 + wave; r < r1; r += 4) {
       const float f = bias && bias[r] == neg_inf() ? 0.f : (factor ? factor[r] : 1.f);
       float v[V];
-      load_piece(x + r * d, t, d, vec, v);
+      load_piece(x + r * d, t, d, v);
 #pragma unroll
       for (int i = 0; i < V; ++i) mx[i] = f != 0.f ? fmaxf(mx[i], fabsf(v[i]) * f) : mx[i];
     }
@@ -817,22 +827,26 @@ __global__ __launch_bounds__(256) void sm_colmax_kernel(const typename Elem<DT>:
 
 // 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r, read and written in 16-byte pieces
 template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void sm_prep_cols_kernel(const typename Elem<DT>::T* __restrict__ x, int64_t n, int d,
-                                                           int64_t np, const float* __restrict__ bias,
-                                                           const float* __restrict__ factor, const u32* __restrict__ colmax,
-                                                           char* __restrict__ planes, float* __restrict__ scale) {
+__global__ __launch_bounds__(256) void sm_prep_cols_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d) {
   typedef typename Elem<DT>::T T;
   constexpr int V = 16 / sizeof(T);
   __shared__ float tile[64][65];
-  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const SmSide& S = blockIdx.x < blocks0 ? side0 : side1;
+  const T* __restrict__ x = static_cast<const T*>(S.x);
+  const float* __restrict__ bias = S.bias;
+  const float* __restrict__ factor = S.factor;
+  const u32* __restrict__ colmax = S.colmax;
+  char* __restrict__ planes = static_cast<char*>(S.cols);
+  float* __restrict__ scale = S.col_scale;
+  const int64_t n = S.n, np = S.np;
+  const int64_t r0 = (int64_t)(blockIdx.x < blocks0 ? blockIdx.x : blockIdx.x - blocks0) * 64;
   const int t0 = blockIdx.y * 64;
-  const bool vec = d % V == 0;
   for (int i = threadIdx.x; i < 64 * 64 / V; i += 256) {
     const int row = i / (64 / V), c = i % (64 / V) * V;
     const int64_t r = r0 + row;
     float v[V] = {};
     const float f = r < n && !(bias && bias[r] == neg_inf()) ? (factor ? factor[r] : 1.f) : 0.f;
-    if (f != 0.f && t0 + c < d) load_piece(x + r * d, t0 + c, d, vec, v);
+    if (f != 0.f && t0 + c < d) load_piece(x + r * d, t0 + c, d, v);
 #pragma unroll
     for (int u = 0; u < V; ++u) tile[row][c + u] = f != 0.f ? v[u] * f : 0.f;   // (what takes no part may be a NaN)
   }
@@ -857,14 +871,15 @@ __global__ __launch_bounds__(256) void sm_prep_cols_kernel(const typename Elem<D
       *reinterpret_cast<f16x8*>(out + (kk >> 4) * 64 + (kk & 15) * 2) = hi;
       *reinterpret_cast<f16x8*>(out + (kk >> 4) * 64 + 32 + (kk & 15) * 2) = lo;
     }
-    if (blockIdx.x == 0 && k == 0) scale[t] = down;
+    if (r0 == 0 && k == 0) scale[t] = down;
   }
 }
 
 // ---- backward ------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, int64_t nb, float4* __restrict__ coef,
-                                                       float* __restrict__ bound) {
+                                                       float* __restrict__ bound, u32* __restrict__ clear, int n_clear) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  for (int64_t c = i; c < n_clear; c += (int64_t)gridDim.x * 256) clear[c] = 0;
   if (i >= nq) return;
   float sum = 0.f, mag = 0.f;
   if (g.g_logp)
@@ -888,24 +903,25 @@ __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, in
 
 // Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
 // G / bound 2^14 in fp16: a value keeps 11 bits (22 with a tail) down to 2^-28 of the bound and 2^-38 of it below.
-template <int PLANES, bool BF16>
+template <int PLANES, bool BF16, int IB, int JB>
 __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut O, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   tile_of(blockIdx.x, ta, tb, &ia, &ib_);
-  const int64_t a0 = ia * kTileA, b0 = ib_ * kTileB;
-  f32x16 acc[4][2] = {};
-  TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
+  constexpr int TA = 64 * IB, TB = 64 * JB;
+  const int64_t a0 = ia * TA, b0 = ib_ * TB;
+  f32x16 acc[IB][JB] = {};
+  TileMul<PLANES, BF16, IB, JB>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
   finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
-  for (int jb = 0; jb < 2; ++jb) {
-    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
     const bool in = qi < S.nq;
     const float4 c = in ? O.coef[qi] : make_float4(0.f, 0.f, 0.f, neg_inf());
     const bool some = c.w != neg_inf();
 #pragma unroll
-    for (int ib = 0; ib < 4; ++ib)
+    for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float s = acc[ib][jb][r];
@@ -916,106 +932,108 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
       }
     if (O.g_logp && in)
       for (int t = 0; t < O.nt; ++t) {
-        const int64_t j = O.targets[qi * O.nt + t] - O.row0 - a0 - wa * 128;  // relative to the wavefront's rows
-        if (j >= 0 && j < 128) {
+        const int64_t j = O.targets[qi * O.nt + t] - O.row0 - a0 - wa * 32 * IB;  // relative to the wavefront's rows
+        if (j >= 0 && j < 32 * IB) {
           const float gl = O.g_logp[qi * O.nt + t];
 #pragma unroll
-          for (int ib = 0; ib < 4; ++ib)
+          for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if ((int)j == ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) acc[ib][jb][r] += gl;
         }
       }
 #pragma unroll
-    for (int ib = 0; ib < 4; ++ib)
+    for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[ib][jb][r] = acc[ib][jb][r] == neg_inf() ? 0.f : acc[ib][jb][r];
   }
   __syncthreads();                                                  // (rowdata has been read)
   if (O.db) {                                                       // column sums of this tile, in a fixed order
-    float* dbs = reinterpret_cast<float*>(lds);                     // [2][256]
+    float* dbs = reinterpret_cast<float*>(lds);                     // [2][TA]
 #pragma unroll
-    for (int ib = 0; ib < 4; ++ib)
+    for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float v = acc[ib][0][r] + acc[ib][1][r];
+        float v = acc[ib][0][r] + (JB == 2 ? acc[ib][JB - 1][r] : 0.f);
         v += __uint_as_float(lane_xor_u32<1>(__float_as_uint(v)));
         v += __uint_as_float(lane_xor_u32<2>(__float_as_uint(v)));
         v += __uint_as_float(lane_xor_u32<4>(__float_as_uint(v)));
         v += __uint_as_float(lane_xor_u32<8>(__float_as_uint(v)));
         v += __shfl_xor(v, 16);
-        if ((lane & 31) == 0) dbs[wb * 256 + wa * 128 + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half] = v;
+        if ((lane & 31) == 0) dbs[wb * TA + (wa * IB + ib) * 32 + (r & 3) + 8 * (r >> 2) + 4 * half] = v;
       }
     __syncthreads();
-    if (a0 + threadIdx.x < S.nx) O.db[ib_ * O.db_ld + a0 + threadIdx.x] = dbs[threadIdx.x] + dbs[256 + threadIdx.x];
+    if (threadIdx.x < TA && a0 + threadIdx.x < S.nx)
+      O.db[ib_ * O.db_ld + a0 + threadIdx.x] = dbs[threadIdx.x] + dbs[TA + threadIdx.x];
     __syncthreads();
   }
 #pragma unroll
-  for (int jb = 0; jb < 2; ++jb) {
-    const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
     const float bnd = qi < S.nq ? O.bound[qi] : 0.f;
     const float inv = bnd == 0.f ? 0.f : 16384.f / bnd;
 #pragma unroll
-    for (int ib = 0; ib < 4; ++ib)
+    for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[ib][jb][r] *= inv;
   }
-  // Out through LDS, 128 rows by 128 queries at a time: the wavefronts of one half of the rows write, all copy.
-  constexpr int LD = 2 * 128 + 16;                                  // bytes of a row of the staged tile
+  // Out through LDS, 128 rows at a time: the wavefronts that hold them write, all copy.
+  constexpr int LDG = 2 * 128 + 16, LDT = 2 * TB + 16;              // bytes of a row of the staged tiles
   constexpr int PER = PLANES == 2 ? 16 : 32;                        // elements of a K unit
   for (int plane = 0; plane < PLANES; ++plane) {
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < TA / 128; ++h) {
       const int64_t x0 = a0 + h * 128;
       if (O.g) {
         // rows of G: queries; four consecutive rows of x are 8 bytes of it
-        if (wa == h) {
+        if (IB == 2 || wa == h) {
 #pragma unroll
-          for (int jb = 0; jb < 2; ++jb)
+          for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-            for (int ib = 0; ib < 4; ++ib)
+            for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
               for (int r = 0; r < 16; r += 4) {
                 f16x4 v;
 #pragma unroll
                 for (int u = 0; u < 4; ++u) v[u] = (_Float16)acc[ib][jb][r + u];
-                *reinterpret_cast<f16x4*>(lds + (wb * 64 + jb * 32 + (lane & 31)) * LD + 2 * (ib * 32 + 2 * r + 4 * half)) = v;
+                *reinterpret_cast<f16x4*>(lds + ((wb * JB + jb) * 32 + (lane & 31)) * LDG +
+                                          2 * ((IB == 2 ? wa * 64 : 0) + ib * 32 + 2 * r + 4 * half)) = v;
               }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < 128 * 16; i += 256) {
+        for (int i = threadIdx.x; i < TB * 16; i += 256) {
           const int row = i >> 4, k = (i & 15) * 8;                 // 8 elements
           if (b0 + row < S.nq)
             *reinterpret_cast<u32x4*>(static_cast<char*>(O.g) + (b0 + row) * O.g_row_bytes + (x0 + k) / PER * 64 + plane * 32 +
-                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LDG + 2 * k);
         }
         __syncthreads();
       }
       if (O.gt) {
-        if (wa == h) {
+        if (IB == 2 || wa == h) {
 #pragma unroll
-          for (int jb = 0; jb < 2; ++jb)
+          for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-            for (int ib = 0; ib < 4; ++ib)
+            for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
               for (int r = 0; r < 16; ++r)
-                *reinterpret_cast<_Float16*>(lds + (ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) * LD +
-                                             2 * (wb * 64 + jb * 32 + (lane & 31))) = (_Float16)acc[ib][jb][r];
+                *reinterpret_cast<_Float16*>(lds + ((IB == 2 ? wa * 64 : 0) + ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half) * LDT +
+                                             2 * ((wb * JB + jb) * 32 + (lane & 31))) = (_Float16)acc[ib][jb][r];
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < 128 * 16; i += 256) {
-          const int row = i >> 4, k = (i & 15) * 8;
+        for (int i = threadIdx.x; i < 128 * (TB / 8); i += 256) {
+          const int row = i / (TB / 8), k = i % (TB / 8) * 8;
           if (x0 + row < S.nx)
             *reinterpret_cast<u32x4*>(static_cast<char*>(O.gt) + (x0 + row) * O.gt_row_bytes + (b0 + k) / PER * 64 + plane * 32 +
-                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LD + 2 * k);
+                                      (k % PER) * 2) = *reinterpret_cast<const u32x4*>(lds + row * LDT + 2 * k);
         }
         __syncthreads();
       }
     }
     if (PLANES == 2 && plane == 0) {
 #pragma unroll
-      for (int jb = 0; jb < 2; ++jb)
+      for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-        for (int ib = 0; ib < 4; ++ib)
+        for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[ib][jb][r] -= (float)(_Float16)acc[ib][jb][r];
     }
@@ -1159,7 +1177,7 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
   }
 }
 
-// The same on the tiles of the scores, for products that give 256 x 256 tiles too few workgroups.  K in units.
+// The same on tiles of 128 x 64, for products that give 256 x 256 tiles too few workgroups.  K in units.
 template <int PLANES>
 __global__ __launch_bounds__(256, 2) void sm_product_small_kernel(SmMatrix A, SmMatrix B, int64_t kunits, int splits, int add,
                                                                   float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb) {
@@ -1168,21 +1186,22 @@ __global__ __launch_bounds__(256, 2) void sm_product_small_kernel(SmMatrix A, Sm
   const int64_t tiles = ta * tb;
   const int split = (int)(blockIdx.x / tiles);
   tile_of(blockIdx.x - split * tiles, ta, tb, &ia, &ib_);
-  const int64_t a0 = ia * kTileA, b0 = ib_ * kTileB;
+  constexpr int IB = 2, JB = 1;
+  const int64_t a0 = ia * 64 * IB, b0 = ib_ * 64 * JB;
   const int64_t k0 = kunits * split / splits, k1 = kunits * (split + 1) / splits;
-  f32x16 acc[4][2] = {};
-  if (k1 > k0) TileMul<PLANES, false>::run(A, a0, B, b0, k0, k1, lds, acc);
+  f32x16 acc[IB][JB] = {};
+  if (k1 > k0) TileMul<PLANES, false, IB, JB>::run(A, a0, B, b0, k0, k1, lds, acc);
   const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
-  for (int jb = 0; jb < 2; ++jb) {
-    const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t b = b0 + (wb * JB + jb) * 32 + (lane & 31);
     if (b >= B.rows) continue;
     float* out = part + (split * B.rows + b) * ld;
 #pragma unroll
-    for (int ib = 0; ib < 4; ++ib)
+    for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const int64_t a = a0 + wa * 128 + ib * 32 + 2 * r + 4 * half;
+        const int64_t a = a0 + (wa * IB + ib) * 32 + 2 * r + 4 * half;
         if (a >= ld) continue;
         float4 v = make_float4(acc[ib][jb][r], acc[ib][jb][r + 1], acc[ib][jb][r + 2], acc[ib][jb][r + 3]);
         float4* o = reinterpret_cast<float4*>(out + a);
@@ -1225,8 +1244,7 @@ __global__ __launch_bounds__(64) void sm_zero_bytes_kernel(unsigned char* __rest
   if ((int)threadIdx.x < n) p[threadIdx.x] = 0;
 }
 
-inline int64_t tiles_a(int64_t n) { return (n + kTileA - 1) / kTileA; }
-inline int64_t tiles_b(int64_t n) { return (n + kTileB - 1) / kTileB; }
+inline int64_t tiles(int64_t n, int per) { return (n + per - 1) / per; }
 inline unsigned grid_of(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
 }  // namespace
@@ -1240,46 +1258,41 @@ void launch_sm_zero(void* p, int64_t bytes, hipStream_t st) {
   if (bytes & 3) sm_zero_bytes_kernel<<<1, 64, 0, st>>>(static_cast<unsigned char*>(p) + words * 4, (int)(bytes & 3));
 }
 
-void launch_sm_prep_rows(const SmForm& f, const void* x, int64_t n, int d, const float* bias, void* planes, float* scale,
-                         hipStream_t st) {
-  if (n == 0) return;
+void launch_sm_prep_rows(const SmForm& f, const SmSide& a, const SmSide& b, int d, hipStream_t st) {
   const int64_t dp = f.blocks(d) * f.per_block();
-  const unsigned g = grid_of(n, 16);
-  if (f.dtype == 0)
-    sm_prep_rows_kernel<0, 2><<<g, 256, 0, st>>>(static_cast<const float*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
-  else if (f.dtype == 1)
-    sm_prep_rows_kernel<1, 1><<<g, 256, 0, st>>>(static_cast<const _Float16*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
-  else
-    sm_prep_rows_kernel<2, 1><<<g, 256, 0, st>>>(static_cast<const __bf16*>(x), n, d, dp, bias, static_cast<char*>(planes), scale);
+  const unsigned ga = grid_of(a.n, 16), g = ga + grid_of(b.n, 16);
+  if (g == 0) return;
+  if (f.dtype == 0) sm_prep_rows_kernel<0, 2><<<g, 256, 0, st>>>(a, b, ga, d, dp);
+  else if (f.dtype == 1) sm_prep_rows_kernel<1, 1><<<g, 256, 0, st>>>(a, b, ga, d, dp);
+  else sm_prep_rows_kernel<2, 1><<<g, 256, 0, st>>>(a, b, ga, d, dp);
 }
 
 namespace {
 template <int DT, int PLANES>
-void prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor, u32* colmax,
-               void* planes, float* scale, hipStream_t st) {
+void prep_cols(SmSide a, SmSide b, const SmForm& f, int d, hipStream_t st) {
   typedef typename Elem<DT>::T T;
-  const int64_t np = f.blocks(n) * f.per_block();
-  const unsigned gy = (unsigned)(n < 64 * 256 ? (n + 63) / 64 : 256);
-  const int64_t per = (n + gy - 1) / gy;
-  launch_sm_zero(colmax, (int64_t)d * 4, st);
-  sm_colmax_kernel<DT><<<dim3(grid_of(d, 64 * 16 / (int)sizeof(T)), gy), 256, 0, st>>>(static_cast<const T*>(x), n, d, bias, factor, per, colmax);
-  sm_prep_cols_kernel<DT, PLANES><<<dim3(grid_of(np, 64), grid_of(d, 64)), 256, 0, st>>>(
-      static_cast<const T*>(x), n, d, np, bias, factor, colmax, static_cast<char*>(planes), scale);
+  a.np = f.blocks(a.n) * f.per_block();
+  b.np = f.blocks(b.n) * f.per_block();
+  const int64_t most = a.n > b.n ? a.n : b.n;
+  const int64_t per = most < 64 * 256 ? 64 : (most + 255) / 256;
+  const unsigned ya = grid_of(a.n, (int)per), y = ya + grid_of(b.n, (int)per);
+  sm_colmax_kernel<DT><<<dim3(grid_of(d, 64 * 16 / (int)sizeof(T)), y), 256, 0, st>>>(a, b, ya, d, per);
+  const unsigned xa = grid_of(a.np, 64), x = xa + grid_of(b.np, 64);
+  sm_prep_cols_kernel<DT, PLANES><<<dim3(x, grid_of(d, 64)), 256, 0, st>>>(a, b, xa, d);
 }
 }  // namespace
 
-void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor,
-                         u32* colmax, void* planes, float* scale, hipStream_t st) {
-  if (n == 0) return;
-  if (f.dtype == 0) prep_cols<0, 2>(f, x, n, d, bias, factor, colmax, planes, scale, st);
-  else if (f.dtype == 1) prep_cols<1, 1>(f, x, n, d, bias, factor, colmax, planes, scale, st);
-  else prep_cols<2, 1>(f, x, n, d, bias, factor, colmax, planes, scale, st);
+void launch_sm_prep_cols(const SmForm& f, const SmSide& a, const SmSide& b, int d, hipStream_t st) {
+  if (a.n == 0 && b.n == 0) return;
+  if (f.dtype == 0) prep_cols<0, 2>(a, b, f, d, st);
+  else if (f.dtype == 1) prep_cols<1, 1>(a, b, f, d, st);
+  else prep_cols<2, 1>(a, b, f, d, st);
 }
 
 void launch_sm_scores(const SmForm& f, bool direct, const SmScores& s, const SmRecords& r, bool second, hipStream_t st) {
-  const int64_t ta = tiles_a(s.nx), tb = tiles_b(s.nq);
+  const int64_t ta = tiles(s.nx, kTileA), tb = tiles(s.nq, kTileB);
   const unsigned g = (unsigned)(ta * tb);
-  auto run = [&](auto kern) { kern<<<g, 256, kTileLds, st>>>(s, r, ta, tb); };
+  auto run = [&](auto kern) { kern<<<g, 256, tile_lds<4, 2>(), st>>>(s, r, ta, tb); };
   if (f.planes == 2) { if (second) run(sm_scores_kernel<2, false, true>); else run(sm_scores_kernel<2, false, false>); }
   else if (direct && f.dtype == 2) { if (second) run(sm_scores_kernel<1, true, true>); else run(sm_scores_kernel<1, true, false>); }
   else { if (second) run(sm_scores_kernel<1, false, true>); else run(sm_scores_kernel<1, false, false>); }
@@ -1327,16 +1340,31 @@ void launch_sm_finish(const SmFinish& f, const SmRecords& r, hipStream_t st) {
   else run(sm_finish_kernel<2, true>, sm_finish_kernel<2, false>);
 }
 
-void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, hipStream_t st) {
-  sm_coefs_kernel<<<grid_of(nq, 256), 256, 0, st>>>(g, nq, nb, coef, bound);
+void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, u32* clear, int n_clear, hipStream_t st) {
+  sm_coefs_kernel<<<grid_of(nq, 256), 256, 0, st>>>(g, nq, nb, coef, bound, clear, n_clear);
 }
 
+// Few big tiles leave most CUs without one, and each of them alone with its epilogue: 1024 x 1024 x 96 in fp32 took 40 us
+// on 32 tiles of 256 x 128.
+bool sm_gradients_small(int64_t nx, int64_t nq) { return tiles(nx, kTileA) * tiles(nq, kTileB) < 256; }
+
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st) {
-  const int64_t ta = tiles_a(s.nx), tb = tiles_b(s.nq);
-  const unsigned g = (unsigned)(ta * tb);
-  if (f.planes == 2) sm_gradients_kernel<2, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
-  else if (direct && f.dtype == 2) sm_gradients_kernel<1, true><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
-  else sm_gradients_kernel<1, false><<<g, 256, kTileLds, st>>>(s, o, ta, tb);
+  auto run = [&](auto kern, int ib, int jb, int lds) {
+    const int64_t ta = tiles(s.nx, 64 * ib), tb = tiles(s.nq, 64 * jb);
+    kern<<<(unsigned)(ta * tb), 256, lds, st>>>(s, o, ta, tb);
+  };
+  if (o.small) {
+    constexpr int lds = 64 * (2 * 128 + 16) > 128 * (2 * 64 + 16) ? 64 * (2 * 128 + 16) : 128 * (2 * 64 + 16);
+    const int n = tile_lds<2, 1>() > lds ? tile_lds<2, 1>() : lds;
+    if (f.planes == 2) run(sm_gradients_kernel<2, false, 2, 1>, 2, 1, n);
+    else if (direct && f.dtype == 2) run(sm_gradients_kernel<1, true, 2, 1>, 2, 1, n);
+    else run(sm_gradients_kernel<1, false, 2, 1>, 2, 1, n);
+  } else {
+    const int n = tile_lds<4, 2>();
+    if (f.planes == 2) run(sm_gradients_kernel<2, false, 4, 2>, 4, 2, n);
+    else if (direct && f.dtype == 2) run(sm_gradients_kernel<1, true, 4, 2>, 4, 2, n);
+    else run(sm_gradients_kernel<1, false, 4, 2>, 4, 2, n);
+  }
 }
 
 // Splits of K that give a product some 256 workgroups, eight 128-byte blocks each at least; big: tiles of 256 x 256, where
@@ -1346,7 +1374,7 @@ SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
   SmProductPlan p;
   const int64_t big = (rows_a + kBigTile - 1) / kBigTile * ((rows_b + kBigTile - 1) / kBigTile);
   p.big = big >= 48;
-  const int64_t n = p.big ? big : tiles_a(rows_a) * tiles_b(rows_b), most = kblocks / (p.big ? 8 : 4);
+  const int64_t n = p.big ? big : tiles(rows_a, 128) * tiles(rows_b, 64), most = kblocks / (p.big ? 8 : 4);
   int64_t want = p.big ? (256 + n / 2) / n : (512 + n - 1) / n;
   if (want > most) want = most;
   if (want > 16) want = 16;
@@ -1366,10 +1394,10 @@ void launch_sm_product(const SmForm& f, const SmProductPlan& pp, const SmMatrix&
     if (f.planes == 2) run(sm_product_kernel<2, false>);
     else run(sm_product_kernel<1, false>);
   } else {
-    const int64_t ta = tiles_a(A.rows), tb = tiles_b(B.rows);
+    const int64_t ta = tiles(A.rows, 128), tb = tiles(B.rows, 64);
     const unsigned g = (unsigned)(ta * tb * pp.splits);
-    if (f.planes == 2) sm_product_small_kernel<2><<<g, 256, kTileLds, st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
-    else sm_product_small_kernel<1><<<g, 256, kTileLds, st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
+    if (f.planes == 2) sm_product_small_kernel<2><<<g, 256, tile_lds<2, 1>(), st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
+    else sm_product_small_kernel<1><<<g, 256, tile_lds<2, 1>(), st>>>(A, B, 2 * kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb);
   }
 }
 

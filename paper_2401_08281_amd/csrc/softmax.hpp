@@ -27,13 +27,21 @@ struct SmForm {                     // how the rows of a type are multiplied
   int64_t blocks(int64_t k) const { return (k + per_block() - 1) / per_block(); }
 };
 
-// planes[r] <- the row as K blocks of fp16 parts times 1 / scale[r], the largest component in [128, 256); rows whose
-// bias is -inf become zeros.
-void launch_sm_prep_rows(const SmForm& f, const void* x, int64_t n, int d, const float* bias, void* planes,
-                         float* scale, hipStream_t st);
-// planes[t] <- column t of (factor[r] x[r]) as K blocks over r, times 1 / scale[t]; colmax: [d] u32 of scratch
-void launch_sm_prep_cols(const SmForm& f, const void* x, int64_t n, int d, const float* bias, const float* factor,
-                         u32* colmax, void* planes, float* scale, hipStream_t st);
+// A matrix [n, d] to be prepared; two go in one launch (n = 0: none).
+struct SmSide {
+  const void* x = nullptr;
+  int64_t n = 0;
+  const float* bias = nullptr;      // rows whose bias is -inf become zeros
+  const float* factor = nullptr;    // of every row, for its columns; a row of factor 0 is not read
+  void* rows = nullptr;             // out: every row as K blocks of fp16 parts times 1 / row_scale, its largest component in
+  float* row_scale = nullptr;       // [128, 256)
+  void* cols = nullptr;             // out: every column of (factor x) as K blocks over the rows, likewise
+  float* col_scale = nullptr;
+  u32* colmax = nullptr;            // [d] of scratch, zeros on entry
+  int64_t np = 0;                   // (rows in whole K blocks)
+};
+void launch_sm_prep_rows(const SmForm& f, const SmSide& a, const SmSide& b, int d, hipStream_t st);
+void launch_sm_prep_cols(const SmForm& f, const SmSide& a, const SmSide& b, int d, hipStream_t st);
 
 struct SmScores {                   // s = scale <q, x> + bias for rows x0 .. x0 + nx of x
   SmMatrix x, q;
@@ -63,14 +71,16 @@ struct SmGrads {
   const float* lse; const float* entropy; const int64_t* targets; int nt;
   const float* g_logp; const float* g_lse; const float* g_entropy;
 };
-// coef[i] = {coefficient of p, g_entropy, entropy, lse}, bound[i]: a power of two that no |G_ij| exceeds
-void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, hipStream_t st);
+// coef[i] = {coefficient of p, g_entropy, entropy, lse}, bound[i]: a power of two that no |G_ij| exceeds; clear <- zeros
+void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, float* bound, u32* clear, int n_clear, hipStream_t st);
 struct SmGOut {
   const float4* coef; const float* bound; const int64_t* targets; int nt; const float* g_logp; int64_t row0;
   void* g; int64_t g_row_bytes;     // [nq][K blocks over the rows], or null
   void* gt; int64_t gt_row_bytes;   // [nx][K blocks over the queries], or null
   float* db; int64_t db_ld;         // [query tiles, db_ld] partial column sums, or null
+  bool small;                       // tiles of 128 rows by 64 queries (256 by 128)
 };
+bool sm_gradients_small(int64_t nx, int64_t nq);
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st);
 // out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over workgroups: part[split][b][ld]
 struct SmProductPlan { bool big; int splits; };

@@ -80,8 +80,8 @@ LogprobPlan logprob_plan(int64_t nb, int64_t nq, int d, int dtype, int k) {
 
 struct GradPlan {
   SmForm f;
-  bool direct;
-  int64_t kblocks, row_bytes, chunk, ld, g_row, gt_row, xt_row, qt_row;
+  bool direct, small;
+  int64_t tile_q, kblocks, row_bytes, chunk, ld, g_row, gt_row, xt_row, qt_row;
   SmProductPlan to_q, to_x;
   int64_t o_x, o_xs, o_q, o_qs, o_xt, o_xts, o_qt, o_qts, o_cm, o_coef, o_bound, o_g, o_gt, o_dq, o_dx, o_db, bytes;
 };
@@ -95,6 +95,8 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   const int64_t el = 2 * p.f.planes;
   const int64_t nqp = round_up(nq, kSmTileQueries), nbp = round_up(nb, kSmTileRows);
   p.chunk = std::min(nbp, std::max<int64_t>(kSmTileRows, kPieceBytes / (2 * el * nqp) / kSmTileRows * kSmTileRows));
+  p.small = sm_gradients_small(p.chunk, nq);
+  p.tile_q = p.small ? 64 : kSmTileQueries;
   p.ld = round_up(d, 4);
   p.g_row = p.chunk * el;
   p.gt_row = nqp * el;
@@ -113,14 +115,14 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   p.o_xts = c.take((int64_t)d * 4);
   p.o_qt = c.take(d * p.qt_row);
   p.o_qts = c.take((int64_t)d * 4);
-  p.o_cm = c.take((int64_t)d * 4);
+  p.o_cm = c.take((int64_t)d * 8);
   p.o_coef = c.take(nq * (int64_t)sizeof(float4));
   p.o_bound = c.take(nq * 4);
   p.o_g = c.take(nq * p.g_row);
   p.o_gt = c.take(p.chunk * p.gt_row);
   p.o_dq = c.take(p.to_q.splits * nq * p.ld * 4);
   p.o_dx = c.take(!p.to_x.big || p.to_x.splits > 1 ? p.to_x.splits * p.chunk * p.ld * 4 : 0);
-  p.o_db = c.take(nqp / kSmTileQueries * p.chunk * 4);
+  p.o_db = c.take(nqp / p.tile_q * p.chunk * 4);
   p.bytes = c.off;
   return p;
 }
@@ -230,10 +232,12 @@ int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq, int32_
   s.x = SmMatrix{x, p.row_bytes, nb, nullptr};
   s.q = SmMatrix{q, p.row_bytes, nq, nullptr};
   if (!p.few && !p.direct && nb > 0) {
-    launch_sm_prep_rows(p.f, x, nb, d, bias, ws + p.o_x, reinterpret_cast<float*>(ws + p.o_xs), st);
-    launch_sm_prep_rows(p.f, q, nq, d, nullptr, ws + p.o_q, reinterpret_cast<float*>(ws + p.o_qs), st);
-    s.x = SmMatrix{ws + p.o_x, p.row_bytes, nb, reinterpret_cast<float*>(ws + p.o_xs)};
-    s.q = SmMatrix{ws + p.o_q, p.row_bytes, nq, reinterpret_cast<float*>(ws + p.o_qs)};
+    SmSide sx, sq;
+    sx.x = x; sx.n = nb; sx.bias = bias; sx.rows = ws + p.o_x; sx.row_scale = reinterpret_cast<float*>(ws + p.o_xs);
+    sq.x = q; sq.n = nq; sq.rows = ws + p.o_q; sq.row_scale = reinterpret_cast<float*>(ws + p.o_qs);
+    launch_sm_prep_rows(p.f, sx, sq, d, st);
+    s.x = SmMatrix{sx.rows, p.row_bytes, nb, sx.row_scale};
+    s.q = SmMatrix{sq.rows, p.row_bytes, nq, sq.row_scale};
   }
   SmRecords r;
   r.rec = reinterpret_cast<float4*>(ws + p.o_rec);
@@ -288,28 +292,34 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     return fail(VS_ERR_INVALID_ARG, "%s: x and q have to be 16-byte aligned, their gradients 4-byte", who);
   const GradPlan p = grad_plan(nb, nq, d, dtype);
   if (int rc = check_space(who, workspace, workspace_bytes, p.bytes)) return rc;
-  const int64_t tq = (nq + kSmTileQueries - 1) / kSmTileQueries;
-  if (tq * (p.chunk / kSmTileRows) >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  if ((nq + 63) / 64 * (p.chunk / kSmTileRows) >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
   if (!out_dq && !out_dx && !out_dbias) return VS_OK;
   char* ws = static_cast<char*>(workspace);
   auto at = [&](int64_t o) { return reinterpret_cast<float*>(ws + o); };
   const SmForm prod{VS_FP16, p.f.planes};                    // the operands of the two products are fp16 parts
   float* bound = at(p.o_bound);
   SmGrads g{lse, entropy, targets, nt, nt > 0 ? g_logp : nullptr, g_lse, g_entropy};
-  launch_sm_coefs(g, nq, nb, reinterpret_cast<float4*>(ws + p.o_coef), bound, st);
+  u32* colmax = reinterpret_cast<u32*>(ws + p.o_cm);
+  launch_sm_coefs(g, nq, nb, reinterpret_cast<float4*>(ws + p.o_coef), bound, colmax, 2 * d, st);
+  SmSide sx, sq;
+  sx.x = x; sx.n = nb; sx.bias = bias; sx.rows = ws + p.o_x; sx.row_scale = at(p.o_xs);
+  sx.cols = ws + p.o_xt; sx.col_scale = at(p.o_xts); sx.colmax = colmax;
+  sq.x = q; sq.n = nq; sq.factor = bound; sq.rows = ws + p.o_q; sq.row_scale = at(p.o_qs);
+  sq.cols = ws + p.o_qt; sq.col_scale = at(p.o_qts); sq.colmax = colmax + d;
   SmScores s;
   s.kunits = 2 * p.kblocks; s.nq = nq; s.scale = scale;
   const char* xp = static_cast<const char*>(x);
   const float* xs = nullptr;
   s.q = SmMatrix{q, p.row_bytes, nq, nullptr};
   if (!p.direct) {
-    launch_sm_prep_rows(p.f, x, nb, d, bias, ws + p.o_x, at(p.o_xs), st);
-    launch_sm_prep_rows(p.f, q, nq, d, nullptr, ws + p.o_q, at(p.o_qs), st);
+    launch_sm_prep_rows(p.f, sx, sq, d, st);
     xp = ws + p.o_x; xs = at(p.o_xs);
-    s.q = SmMatrix{ws + p.o_q, p.row_bytes, nq, at(p.o_qs)};
+    s.q = SmMatrix{sq.rows, p.row_bytes, nq, sq.row_scale};
   }
-  if (out_dq) launch_sm_prep_cols(p.f, x, nb, d, bias, nullptr, reinterpret_cast<u32*>(ws + p.o_cm), ws + p.o_xt, at(p.o_xts), st);
-  if (out_dx) launch_sm_prep_cols(p.f, q, nq, d, nullptr, bound, reinterpret_cast<u32*>(ws + p.o_cm), ws + p.o_qt, at(p.o_qts), st);
+  SmSide cx = sx, cq = sq;
+  if (!out_dq) cx.n = 0;
+  if (!out_dx) cq.n = 0;
+  launch_sm_prep_cols(p.f, cx, cq, d, st);
   const float alpha = scale * (1.f / 16384.f);
   for (int64_t x0 = 0; x0 < nb; x0 += p.chunk) {
     const int64_t n = std::min(p.chunk, nb - x0);
@@ -318,7 +328,7 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     s.bias = bias ? bias + x0 : nullptr;
     SmGOut o{reinterpret_cast<float4*>(ws + p.o_coef), bound, targets, nt, g.g_logp, x0,
              out_dq ? ws + p.o_g : nullptr, p.g_row, out_dx ? ws + p.o_gt : nullptr, p.gt_row,
-             out_dbias ? at(p.o_db) : nullptr, p.chunk};
+             out_dbias ? at(p.o_db) : nullptr, p.chunk, p.small};
     launch_sm_gradients(p.f, p.direct, s, o, st);
     if (out_dq) {
       const SmMatrix a{ws + p.o_xt + x0 / p.f.per_block() * 128, p.xt_row, d, nullptr}, b{ws + p.o_g, p.g_row, nq, nullptr};
@@ -334,7 +344,7 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
         launch_sm_product_out(at(p.o_dx), p.to_x.splits, n, p.ld, d, at(p.o_qts), nullptr, alpha, dtype, dx, st);
       }
     }
-    if (out_dbias) launch_sm_sum_parts(at(p.o_db), tq, p.chunk, n, out_dbias + x0, st);
+    if (out_dbias) launch_sm_sum_parts(at(p.o_db), (nq + p.tile_q - 1) / p.tile_q, p.chunk, n, out_dbias + x0, st);
   }
   if (out_dq) launch_sm_product_out(at(p.o_dq), p.to_q.splits, nq, p.ld, d, at(p.o_xts), bound, alpha, dtype, out_dq, st);
   return launched(who);
