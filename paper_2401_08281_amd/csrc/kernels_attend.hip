@@ -19,6 +19,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kRound = 1024;        // rows of a round
 constexpr int kSegments = 64;       // lists it may span
 constexpr int kWaves = 4;
+constexpr int kCodeRun = 72;        // bytes of a staged run of 64 rows' codes (18 words: runs start in different banks)
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
 __device__ __forceinline__ float wave_sum(float v) {
@@ -69,10 +70,12 @@ __device__ __forceinline__ void settle_products() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Groups of lanes that a wavefront's 64 rows are shared out to: 1, 2, 4 or 8 (eight rows each at least)
+__device__ __forceinline__ int row_groups(int mh) { return mh > 32 ? 1 : (mh > 16 ? 2 : (mh > 8 ? 4 : 8)); }
+
 // What a workgroup of QB queries keeps in LDS, in floats.
 struct ScanLds {
   int lut, lut2, q, g, score, score2, hist, cacc, codes, bias, bias2, red, seg, total;
-  int code_words;                    // words of a staged code (odd: no two rows start in one bank)
   int mh, mc;                        // histogrammed sub-quantizers; 64-lane chunks of them
 };
 __host__ __device__ inline ScanLds scan_lds(const IvfpqDims& g, int dk, int v0, int qb, bool grad) {
@@ -80,7 +83,6 @@ __host__ __device__ inline ScanLds scan_lds(const IvfpqDims& g, int dk, int v0, 
   const int mk = dk / g.dsub, mv = (g.d - v0) / g.dsub, out = grad ? dk : g.d - v0, sets = grad ? 2 : 1;
   o.mh = grad ? mk : mv;
   o.mc = (o.mh + 63) / 64;
-  o.code_words = ((g.code_size + 3) / 4) | 1;
   int at = 0;
   auto take = [&](int n) { const int o2 = at; at += (n + 3) / 4 * 4; return o2; };
   o.lut = take(mk * 16 * qb);
@@ -91,7 +93,7 @@ __host__ __device__ inline ScanLds scan_lds(const IvfpqDims& g, int dk, int v0, 
   o.score2 = take(grad ? kRound * qb : 0);
   o.hist = take(kWaves * sets * qb * o.mc * 1024);
   o.cacc = take(sets * qb * out);
-  o.codes = take(kWaves * 64 * o.code_words);
+  o.codes = take((kWaves * g.code_size * kCodeRun + 3) / 4);
   o.bias = take(kSegments * qb);
   o.bias2 = take(grad ? kSegments * qb : 0);
   o.red = take(kWaves * 2 * qb + 8);
@@ -122,26 +124,58 @@ __device__ __forceinline__ void look_up(const float* lut, u32 word, int u, float
     acc[0] += e[0];
   }
 }
+// The words of a row, requested together (rows of up to 64 bytes; longer ones are read as they are used)
+constexpr int kRowWords = 16;
+__device__ __forceinline__ void load_row(const uint8_t* row, int cs, u32 (&w)[kRowWords]) {
+  if ((cs & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < kRowWords; i += 4) {
+      u32x4 v = {0, 0, 0, 0};
+      if (i * 4 < cs) __builtin_memcpy(&v, row + i * 4, 16);
+      w[i] = v[0]; w[i + 1] = v[1]; w[i + 2] = v[2]; w[i + 3] = v[3];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRowWords; ++i) w[i] = i * 4 < cs ? code_word(row, i, cs) : 0u;
+  }
+}
+
 // Sum of the look-ups of sub-quantizers [m0, m1) of one row, in two chains: half the roundings in a row, and no addition
 // waits for the one before.  The bias, usually the largest term, comes last.
 template <int QB>
-__device__ __forceinline__ void score_row(const uint8_t* row, int cs, int m0, int m1, const float* lut, const float* bias,
-                                          float (&out)[QB]) {
+__device__ __forceinline__ void score_word(u32 word, int w, int m0, int m1, const float* lut, float (&acc)[2][QB]) {
+  const float* t = lut + (w * 8 - m0) * 16 * QB;
+  if (w * 8 >= m0 && w * 8 + 8 <= m1) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u) look_up<QB>(t, word, u, acc[u & 1]);
+  } else {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (w * 8 + u >= m0 && w * 8 + u < m1) look_up<QB>(t, word, u, acc[u & 1]);
+  }
+}
+template <int QB>
+__device__ __forceinline__ void score_row(const uint8_t* row, const u32 (&words)[kRowWords], int cs, int m0, int m1,
+                                          const float* lut, const float* bias, float (&out)[QB]) {
   float acc[2][QB] = {};
-  for (int w = m0 / 8; w * 8 < m1; ++w) {
-    const u32 word = code_word(row, w, cs);
-    const float* t = lut + (w * 8 - m0) * 16 * QB;
-    if (w * 8 >= m0 && w * 8 + 8 <= m1) {
+  if (cs <= 4 * kRowWords) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u) look_up<QB>(t, word, u, acc[u & 1]);
-    } else {
-#pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (w * 8 + u >= m0 && w * 8 + u < m1) look_up<QB>(t, word, u, acc[u & 1]);
-    }
+    for (int w = 0; w < kRowWords; ++w)
+      if (w * 8 < m1 && w * 8 + 8 > m0) score_word<QB>(words[w], w, m0, m1, lut, acc);
+  } else {
+    for (int w = m0 / 8; w * 8 < m1; ++w) score_word<QB>(code_word(row, w, cs), w, m0, m1, lut, acc);
   }
 #pragma unroll
   for (int b = 0; b < QB; ++b) out[b] = (acc[0][b] + acc[1][b]) + bias[b];
+}
+
+// Two rows' weights into one column of a histogram: both cells are read before either is written; where the codes are
+// equal both writes carry the sum.
+__device__ __forceinline__ void add_pair(float* h, u32 c0, u32 c1, float p0, float p1) {
+  const float v0 = h[c0 * 64], v1 = h[c1 * 64];
+  const float s0 = v0 + p0, s1 = (c0 == c1 ? s0 : v1) + p1;
+  h[c0 * 64] = s0;
+  h[c1 * 64] = s1;                          // (after the first: with equal codes this one stays)
 }
 
 template <int QB, bool GRAD>
@@ -216,8 +250,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     if (GRAD && lse[b] == neg_inf()) limit[b] = INT64_MIN;      // saw nothing
     mx[b] = neg_inf(); sum[b] = 0.f; sum2[b] = 0.f; shift[b] = 0.f;
   }
-  const int rs = lane / (L.mh < 64 ? L.mh : 64), hm = lane % (L.mh < 64 ? L.mh : 64);
-  const int rstep = L.mh < 64 ? 64 / L.mh : 1;
+  const int rstep = row_groups(L.mh), rs = lane / (L.mh < 64 ? L.mh : 64), hm = lane % (L.mh < 64 ? L.mh : 64);
   const bool hist_lane = rs < rstep;
 
   while (true) {
@@ -303,8 +336,11 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
           const int64_t pos = sg.pos + i;
           const int64_t id = A.limits ? A.ids[pos] : 0;
           float acc[QB], acc2[QB];
-          score_row<QB>(A.codes + pos * cs, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
-          if (GRAD) score_row<QB>(A.codes + pos * cs, cs, mv0, M, lds + L.lut2, lds + L.bias2 + s * QB, acc2);
+          const uint8_t* row = A.codes + pos * cs;
+          u32 words[kRowWords];
+          if (cs <= 4 * kRowWords) load_row(row, cs, words);
+          score_row<QB>(row, words, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
+          if (GRAD) score_row<QB>(row, words, cs, mv0, M, lds + L.lut2, lds + L.bias2 + s * QB, acc2);
 #pragma unroll
           for (int b = 0; b < QB; ++b) {
             const bool sees = id < limit[b];
@@ -398,38 +434,55 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
         }
       }
     }
-    // histograms: a wavefront takes 64 rows, brings their codes into LDS, and adds row by row
+    // histograms: a wavefront takes 64 rows, turns their codes round in LDS (byte m / 2 of 64 rows in a run) and adds them
+    // eight rows at a time; its groups of lanes, if sub-quantizers leave room for several, take a part of the rows each
     tile = 0;
     for (int s = 0; s < nseg; ++s) {
       const Segment sg = segs[s];
       for (int t0 = 0; t0 < sg.len; t0 += 64, ++tile) {
         if ((tile & (kWaves - 1)) != wave) continue;
         const int n = sg.len - t0 < 64 ? sg.len - t0 : 64;
-        u32* ct = reinterpret_cast<u32*>(lds + L.codes) + wave * 64 * L.code_words;
+        uint8_t* ct = reinterpret_cast<uint8_t*>(lds + L.codes) + wave * cs * kCodeRun;
         wave_lds_sync();
-        if (lane < n) {
-          const uint8_t* row = A.codes + (sg.pos + t0 + lane) * cs;
-          for (int w = 0; w * 4 < cs; ++w) ct[lane * L.code_words + w] = code_word(row, w, cs);
+        {
+          const uint8_t* row = A.codes + (sg.pos + t0 + (lane < n ? lane : 0)) * cs;
+          if (cs <= 4 * kRowWords) {
+            u32 words[kRowWords];
+            load_row(row, cs, words);
+#pragma unroll
+            for (int w = 0; w < kRowWords; ++w)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                if (w * 4 + u < cs) ct[(w * 4 + u) * kCodeRun + lane] = (uint8_t)(words[w] >> (8 * u));
+          } else {
+            for (int i = 0; i < cs; ++i) ct[i * kCodeRun + lane] = row[i];
+          }
         }
         wave_lds_sync();
         if (hist_lane) {
           const float* pr = lds + L.score + (sg.first + t0) * QB;
           const float* pr2 = lds + L.score2 + (sg.first + t0) * QB;
+          const int per = 64 / rstep, j0 = rs * per, j1 = n < j0 + per ? n : j0 + per;
           for (int mc = 0; mc < L.mc; ++mc) {
             const int m = mc * 64 + hm;
             if (m >= L.mh) break;
-            const uint8_t* cb = reinterpret_cast<const uint8_t*>(ct) + (h0 + m) / 2;
+            const uint8_t* cb = ct + (h0 + m) / 2 * kCodeRun;
             const int sh = ((h0 + m) & 1) * 4;
             float* hc = hist + mc * 1024 + lane;
-            for (int j = rs; j < n; j += rstep) {
-              const int c = (cb[j * L.code_words * 4] >> sh) & 15;
+            for (int j = j0; j < j1; j += 8) {
+              u64 c8;
+              __builtin_memcpy(&c8, __builtin_assume_aligned(cb + j, 8), 8);
+              c8 >>= sh;
 #pragma unroll
-              for (int b = 0; b < QB; ++b) {
-                if (GRAD) {
-                  hc[(0 * QB + b) * L.mc * 1024 + c * 64] += pr2[j * QB + b];
-                  hc[(1 * QB + b) * L.mc * 1024 + c * 64] += pr[j * QB + b];
-                } else {
-                  hc[b * L.mc * 1024 + c * 64] += pr[j * QB + b];
+              for (int i = 0; i < 8; i += 2) {
+                const u32 ca = (u32)(c8 >> (8 * i)) & 15u, cc = (u32)(c8 >> (8 * i + 8)) & 15u;
+                // (rows past the end: nothing, wherever their codes point)
+                const bool in0 = j + i < j1, in1 = j + i + 1 < j1;
+                const int at0 = (in0 ? j + i : j0) * QB, at1 = (in1 ? j + i + 1 : j0) * QB;
+#pragma unroll
+                for (int b = 0; b < QB; ++b) {
+                  if (GRAD) add_pair(hc + b * L.mc * 1024, ca, cc, in0 ? pr2[at0 + b] : 0.f, in1 ? pr2[at1 + b] : 0.f);
+                  add_pair(hc + ((SETS - 1) * QB + b) * L.mc * 1024, ca, cc, in0 ? pr[at0 + b] : 0.f, in1 ? pr[at1 + b] : 0.f);
                 }
               }
             }

@@ -1274,7 +1274,7 @@ void prep_cols(SmSide a, SmSide b, const SmForm& f, int d, hipStream_t st) {
   a.np = f.blocks(a.n) * f.per_block();
   b.np = f.blocks(b.n) * f.per_block();
   const int64_t most = a.n > b.n ? a.n : b.n;
-  const int64_t per = most < 64 * 256 ? 64 : (most + 255) / 256;
+  const int64_t per = most < 64 * 1024 ? 64 : (most + 1023) / 1024;
   const unsigned ya = grid_of(a.n, (int)per), y = ya + grid_of(b.n, (int)per);
   sm_colmax_kernel<DT><<<dim3(grid_of(d, 64 * 16 / (int)sizeof(T)), y), 256, 0, st>>>(a, b, ya, d, per);
   const unsigned xa = grid_of(a.np, 64), x = xa + grid_of(b.np, 64);
