@@ -5,10 +5,12 @@
 //   out_i = sum_l P_l c_l + concat_m sum_c H_m[c] T_m[c],  H_m[c] = sum of p_j with code_jm = c  (an addition per one)
 // so a stored vector costs 2 M operations on LDS a query instead of 2 d products, whatever its dimension.
 //
-// A workgroup takes QB queries and a part of the rows, in rounds of up to 1024 rows: scores (one row a lane, all
-// queries), their maximum, weights, then the histograms H (one sub-quantizer a lane).  A lane adds to its own column of
-// its wavefront's H only: additions keep their order, banks never collide.  Partial results of the parts are joined by a
-// second kernel.  Bound by LDS: one look-up of QB values and one addition per query for every code.
+// A workgroup takes QB queries and a part of the rows, in rounds of up to 2048 rows: scores (one row a lane, all
+// queries), their maximum, weights, then the weighted sums (one sub-quantizer a lane).  Codewords of up to four components
+// are looked up whole and added to the lane's registers; longer ones go through the histograms H: a lane adds to its own
+// column of its wavefront's H only, so additions keep their order and banks never collide.  (Additions by LDS atomics ran
+// at 24 cycles a wavefront, three times the whole scan.)  Partial results of the parts are joined by a second kernel.
+// Bound by LDS: one look-up of QB values, and one of a codeword or a histogram cell, for every code.
 #include "../../include/vs_softmax.h"
 #include "common.hpp"
 #include "softmax.hpp"
@@ -16,8 +18,9 @@
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr int kRound = 1024;        // rows of a round
+constexpr int kRound = 2048;        // rows of a round
 constexpr int kSegments = 64;       // lists it may span
+constexpr int kTiles = kRound / 64 + kSegments;   // runs of up to 64 rows of one list
 constexpr int kWaves = 4;
 constexpr int kCodeRun = 72;        // bytes of a staged run of 64 rows' codes (18 words: runs start in different banks)
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -60,7 +63,8 @@ struct ScanArgs {
   int64_t ld;
 };
 
-struct Segment { int64_t pos; int32_t list, first, len, pad; };   // rows [first, first + len) of a round
+struct Segment { int64_t pos; int32_t list, first, len, tile; };   // rows [first, first + len) of a round, its first run
+struct Tile { int64_t pos; int32_t first, len_seg; };              // a run: length, segment << 8
 
 // The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
 // not wait for them, and the compiler does not always count the wait states across the end of a loop.  20 cover any product.
@@ -75,9 +79,14 @@ __device__ __forceinline__ int row_groups(int mh) { return mh > 32 ? 1 : (mh > 1
 
 // What a workgroup of QB queries keeps in LDS, in floats.
 struct ScanLds {
-  int lut, lut2, q, g, score, score2, hist, cacc, codes, bias, bias2, red, seg, total;
+  int lut, lut2, q, g, score, score2, hist, words, cacc, codes, bias, bias2, red, seg, tiles, total;
   int mh, mc;                        // histogrammed sub-quantizers; 64-lane chunks of them
 };
+// Components of a looked-up codeword, padded (0: histograms): where a lane holds one sub-quantizer and 16 bytes hold one
+__host__ __device__ inline int scan_words(const IvfpqDims& g, int dk, int v0, bool grad) {
+  const int mh = (grad ? dk : g.d - v0) / g.dsub;
+  return mh > 64 || g.dsub > 4 ? 0 : (g.dsub > 2 ? 4 : g.dsub);
+}
 __host__ __device__ inline ScanLds scan_lds(const IvfpqDims& g, int dk, int v0, int qb, bool grad) {
   ScanLds o{};
   const int mk = dk / g.dsub, mv = (g.d - v0) / g.dsub, out = grad ? dk : g.d - v0, sets = grad ? 2 : 1;
@@ -91,13 +100,16 @@ __host__ __device__ inline ScanLds scan_lds(const IvfpqDims& g, int dk, int v0, 
   o.g = take(grad ? (g.d - v0) * qb : 0);
   o.score = take(kRound * qb);
   o.score2 = take(grad ? kRound * qb : 0);
-  o.hist = take(kWaves * sets * qb * o.mc * 1024);
+  const int ds = scan_words(g, dk, v0, grad);
+  o.hist = take(ds ? 0 : kWaves * sets * qb * o.mc * 1024);
+  o.words = take(16 * o.mh * ds);
   o.cacc = take(sets * qb * out);
   o.codes = take((kWaves * g.code_size * kCodeRun + 3) / 4);
   o.bias = take(kSegments * qb);
   o.bias2 = take(grad ? kSegments * qb : 0);
   o.red = take(kWaves * 2 * qb + 8);
   o.seg = take((int)(sizeof(Segment) / 4) * kSegments + 8);
+  o.tiles = take((int)(sizeof(Tile) / 4) * kTiles);
   o.total = at;
   return o;
 }
@@ -178,7 +190,7 @@ __device__ __forceinline__ void add_pair(float* h, u32 c0, u32 c1, float p0, flo
   h[c1 * 64] = s1;                          // (after the first: with equal codes this one stays)
 }
 
-template <int QB, bool GRAD>
+template <int QB, bool GRAD, int DS>
 __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   extern __shared__ __align__(16) float lds[];
   const ScanLds L = scan_lds(A.g, A.dk, A.v0, QB, GRAD);
@@ -190,8 +202,9 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   const int split = blockIdx.x % A.nsplit;
   const int64_t q0 = (int64_t)(blockIdx.x / A.nsplit) * QB;
   Segment* segs = reinterpret_cast<Segment*>(lds + L.seg);
-  int* ctl = reinterpret_cast<int*>(lds + L.seg + (int)(sizeof(Segment) / 4) * kSegments);   // {segments, rows, next candidate}
+  int* ctl = reinterpret_cast<int*>(lds + L.seg + (int)(sizeof(Segment) / 4) * kSegments);   // {segments, rows, next candidate, -, offset (two words), runs}
   int64_t* offset = reinterpret_cast<int64_t*>(ctl + 4);         // rows of the next candidate that are done
+  Tile* tiles = reinterpret_cast<Tile*>(lds + L.tiles);
   float* hist = lds + L.hist + wave * SETS * QB * L.mc * 1024;
 
   for (int i = threadIdx.x; i < QB * A.dk; i += 256) {
@@ -203,7 +216,13 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       const int64_t qi = q0 + i / dv;
       lds[L.g + i] = qi < A.nq ? load_as_f32(A.g_out, qi * dv + i % dv, A.dtype) : 0.f;
     }
-  for (int i = threadIdx.x; i < kWaves * SETS * QB * L.mc * 1024; i += 256) lds[L.hist + i] = 0.f;
+  if (DS == 0)
+    for (int i = threadIdx.x; i < kWaves * SETS * QB * L.mc * 1024; i += 256) lds[L.hist + i] = 0.f;
+  // codewords [code][sub-quantizer][DS]: sixteen lanes of consecutive sub-quantizers never share a bank, whatever the codes
+  for (int i = threadIdx.x; i < 16 * L.mh * DS; i += 256) {
+    const int u = i % (DS > 0 ? DS : 1), m = i / (DS > 0 ? DS : 1) % L.mh, c = i / (DS > 0 ? DS : 1) / L.mh;
+    lds[L.words + i] = u < dsub ? A.codebooks[((int64_t)(h0 + m) * 16 + c) * dsub + u] : 0.f;
+  }
   for (int i = threadIdx.x; i < SETS * QB * nout; i += 256) lds[L.cacc + i] = 0.f;
   // the part's rows: candidates are its probes, or the lists that its rows lie in
   int64_t r0 = 0, r1 = 0;
@@ -251,7 +270,8 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     mx[b] = neg_inf(); sum[b] = 0.f; sum2[b] = 0.f; shift[b] = 0.f;
   }
   const int rstep = row_groups(L.mh), rs = lane / (L.mh < 64 ? L.mh : 64), hm = lane % (L.mh < 64 ? L.mh : 64);
-  const bool hist_lane = rs < rstep;
+  const bool hist_lane = rs < rstep && hm < L.mh;
+  float word_sum[SETS][QB][DS > 0 ? DS : 1] = {};
 
   while (true) {
     __syncthreads();
@@ -280,10 +300,19 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       const int first = end - len0;
       const int len = first >= kRound ? 0 : (end > kRound ? kRound - first : len0);
       const u64 taken = __ballot(len > 0);
+      int runs = (len + 63) / 64, run_end = runs;
+#pragma unroll
+      for (int w = 1; w < 64; w <<= 1) {
+        const int o = __shfl_up(run_end, w);
+        if (lane >= w) run_end += o;
+      }
       if (len > 0) {
         const int at = __popcll(taken & ((1ull << lane) - 1));
-        segs[at] = Segment{b, list, first, len, 0};
+        segs[at] = Segment{b, list, first, len, run_end - runs};
+        for (int i = 0; i < runs; ++i)
+          tiles[run_end - runs + i] = Tile{b + i * 64, first + i * 64, (len - i * 64 < 64 ? len - i * 64 : 64) | at << 8};
       }
+      if (lane == 63) ctl[6] = run_end;
       // the next round starts at the first candidate that is not used up
       const u64 open = __ballot(c < c_end && have > len);
       const int stop = open ? __ffsll(open) - 1 : 64;
@@ -295,7 +324,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       }
     }
     __syncthreads();
-    const int nseg = ctl[0], rows = ctl[1], next = ctl[2];
+    const int nseg = ctl[0], rows = ctl[1], next = ctl[2], ntile = ctl[6];
     if (nseg == 0) {
       if (next >= c_end) break;
       continue;
@@ -304,13 +333,19 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     for (int s = wave; s < nseg; s += kWaves) {
       const float* c = A.centroids + (int64_t)segs[s].list * d;
       float v[QB] = {}, v2[QB] = {};
-      for (int t = lane; t < A.dk; t += 64)
+#pragma unroll 4
+      for (int t = lane; t < A.dk; t += 64) {
+        const float ct = c[t];
 #pragma unroll
-        for (int b = 0; b < QB; ++b) v[b] = __builtin_fmaf(lds[L.q + b * A.dk + t], c[t], v[b]);
+        for (int b = 0; b < QB; ++b) v[b] = __builtin_fmaf(lds[L.q + b * A.dk + t], ct, v[b]);
+      }
       if (GRAD)
-        for (int t = lane; t < dv; t += 64)
+#pragma unroll 4
+        for (int t = lane; t < dv; t += 64) {
+          const float ct = c[A.v0 + t];
 #pragma unroll
-          for (int b = 0; b < QB; ++b) v2[b] = __builtin_fmaf(lds[L.g + b * dv + t], c[A.v0 + t], v2[b]);
+          for (int b = 0; b < QB; ++b) v2[b] = __builtin_fmaf(lds[L.g + b * dv + t], ct, v2[b]);
+        }
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
         v[b] = wave_sum(v[b]);
@@ -326,36 +361,43 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     float top[QB], rp[QB], rw[QB];
 #pragma unroll
     for (int b = 0; b < QB; ++b) { top[b] = neg_inf(); rp[b] = 0.f; rw[b] = 0.f; }
-    int tile = 0;
-    for (int s = 0; s < nseg; ++s) {
-      const Segment sg = segs[s];
-      for (int t0 = 0; t0 < sg.len; t0 += 64, ++tile) {
-        if ((tile & (kWaves - 1)) != wave) continue;
-        const int i = t0 + lane;
-        if (i < sg.len) {
-          const int64_t pos = sg.pos + i;
-          const int64_t id = A.limits ? A.ids[pos] : 0;
-          float acc[QB], acc2[QB];
-          const uint8_t* row = A.codes + pos * cs;
-          u32 words[kRowWords];
-          if (cs <= 4 * kRowWords) load_row(row, cs, words);
-          score_row<QB>(row, words, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
-          if (GRAD) score_row<QB>(row, words, cs, mv0, M, lds + L.lut2, lds + L.bias2 + s * QB, acc2);
+    // (the codes of a wavefront's next run are on their way while it looks up the present one)
+    u32 words[kRowWords];
+    int64_t id = 0;
+    auto fetch = [&](int ti) {
+      const Tile tl = tiles[ti];
+      const int64_t pos = tl.pos + (lane < (tl.len_seg & 255) ? lane : 0);
+      if (cs <= 4 * kRowWords) load_row(A.codes + pos * cs, cs, words);
+      if (A.limits) id = A.ids[pos];
+    };
+    if (wave < ntile) fetch(wave);
+    for (int ti = wave; ti < ntile; ti += kWaves) {
+      const Tile tl = tiles[ti];
+      const int s = tl.len_seg >> 8, i = tl.first + lane;
+      u32 now[kRowWords];
 #pragma unroll
-          for (int b = 0; b < QB; ++b) {
-            const bool sees = id < limit[b];
-            if (GRAD) {
-              const float p = sees ? exp_neg(acc[b] - lse[b]) : 0.f;
-              const float w = sees ? p * acc2[b] : 0.f;
-              lds[L.score + (sg.first + i) * QB + b] = p;
-              lds[L.score2 + (sg.first + i) * QB + b] = acc2[b];
-              rp[b] += p;
-              rw[b] += w;
-            } else {
-              const float v = sees ? acc[b] : neg_inf();
-              lds[L.score + (sg.first + i) * QB + b] = v;
-              top[b] = fmaxf(top[b], v);
-            }
+      for (int w = 0; w < kRowWords; ++w) now[w] = words[w];
+      const int64_t my_id = id;
+      if (ti + kWaves < ntile) fetch(ti + kWaves);
+      if (lane < (tl.len_seg & 255)) {
+        float acc[QB], acc2[QB];
+        const uint8_t* row = A.codes + (tl.pos + lane) * cs;
+        score_row<QB>(row, now, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
+        if (GRAD) score_row<QB>(row, now, cs, mv0, M, lds + L.lut2, lds + L.bias2 + s * QB, acc2);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+          const bool sees = my_id < limit[b];
+          if (GRAD) {
+            const float p = sees ? exp_neg(acc[b] - lse[b]) : 0.f;
+            const float w = sees ? p * acc2[b] : 0.f;
+            lds[L.score + i * QB + b] = p;
+            lds[L.score2 + i * QB + b] = acc2[b];
+            rp[b] += p;
+            rw[b] += w;
+          } else {
+            const float v = sees ? acc[b] : neg_inf();
+            lds[L.score + i * QB + b] = v;
+            top[b] = fmaxf(top[b], v);
           }
         }
       }
@@ -379,7 +421,12 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
         sum[b] *= f[b];
       }
       if (grown) {
-        for (int i = threadIdx.x; i < kWaves * QB * L.mc * 1024; i += 256) lds[L.hist + i] *= f[QB == 1 ? 0 : (i / (L.mc * 1024)) % QB];
+        if (DS == 0)
+          for (int i = threadIdx.x; i < kWaves * QB * L.mc * 1024; i += 256) lds[L.hist + i] *= f[QB == 1 ? 0 : (i / (L.mc * 1024)) % QB];
+#pragma unroll
+        for (int b = 0; b < QB; ++b)
+#pragma unroll
+          for (int u = 0; u < (DS > 0 ? DS : 1); ++u) word_sum[0][b][u] *= f[b];
         for (int i = threadIdx.x; i < QB * nout; i += 256) lds[L.cacc + i] *= f[QB == 1 ? 0 : i / nout];
       }
       for (int i = threadIdx.x; i < rows * QB; i += 256) {
@@ -436,33 +483,59 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     }
     // histograms: a wavefront takes 64 rows, turns their codes round in LDS (byte m / 2 of 64 rows in a run) and adds them
     // eight rows at a time; its groups of lanes, if sub-quantizers leave room for several, take a part of the rows each
-    tile = 0;
-    for (int s = 0; s < nseg; ++s) {
-      const Segment sg = segs[s];
-      for (int t0 = 0; t0 < sg.len; t0 += 64, ++tile) {
-        if ((tile & (kWaves - 1)) != wave) continue;
-        const int n = sg.len - t0 < 64 ? sg.len - t0 : 64;
+    if (wave < ntile) fetch(wave);
+    for (int ti = wave; ti < ntile; ti += kWaves) {
+      const Tile tl = tiles[ti];
+      const int n = tl.len_seg & 255;
+      {
         uint8_t* ct = reinterpret_cast<uint8_t*>(lds + L.codes) + wave * cs * kCodeRun;
         wave_lds_sync();
-        {
-          const uint8_t* row = A.codes + (sg.pos + t0 + (lane < n ? lane : 0)) * cs;
-          if (cs <= 4 * kRowWords) {
-            u32 words[kRowWords];
-            load_row(row, cs, words);
+        if (cs <= 4 * kRowWords) {
 #pragma unroll
-            for (int w = 0; w < kRowWords; ++w)
+          for (int w = 0; w < kRowWords; ++w)
 #pragma unroll
-              for (int u = 0; u < 4; ++u)
-                if (w * 4 + u < cs) ct[(w * 4 + u) * kCodeRun + lane] = (uint8_t)(words[w] >> (8 * u));
-          } else {
-            for (int i = 0; i < cs; ++i) ct[i * kCodeRun + lane] = row[i];
-          }
+            for (int u = 0; u < 4; ++u)
+              if (w * 4 + u < cs) ct[(w * 4 + u) * kCodeRun + lane] = (uint8_t)(words[w] >> (8 * u));
+        } else {
+          const uint8_t* row = A.codes + (tl.pos + (lane < n ? lane : 0)) * cs;
+          for (int i = 0; i < cs; ++i) ct[i * kCodeRun + lane] = row[i];
         }
+        if (ti + kWaves < ntile) fetch(ti + kWaves);
         wave_lds_sync();
         if (hist_lane) {
-          const float* pr = lds + L.score + (sg.first + t0) * QB;
-          const float* pr2 = lds + L.score2 + (sg.first + t0) * QB;
+          const float* pr = lds + L.score + tl.first * QB;
+          const float* pr2 = lds + L.score2 + tl.first * QB;
           const int per = 64 / rstep, j0 = rs * per, j1 = n < j0 + per ? n : j0 + per;
+          if constexpr (DS > 0) {
+            typedef float words_t __attribute__((ext_vector_type(DS)));
+            const uint8_t* cb = ct + (h0 + hm) / 2 * kCodeRun;
+            const int sh = ((h0 + hm) & 1) * 4;
+            const float* tab = lds + L.words + hm * DS;
+            for (int j = j0; j < j1; j += 8) {
+              u64 c8;
+              __builtin_memcpy(&c8, __builtin_assume_aligned(cb + j, 8), 8);
+              c8 >>= sh;
+              words_t t[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                t[i] = *reinterpret_cast<const words_t*>(tab + ((u32)(c8 >> (8 * i)) & 15u) * (L.mh * DS));
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const bool in = j + i < j1;              // (rows past the end: nothing, wherever their codes point)
+                const int at = (in ? j + i : j0) * QB;
+#pragma unroll
+                for (int b = 0; b < QB; ++b) {
+                  const float p = in ? pr[at + b] : 0.f, p2 = GRAD && in ? pr2[at + b] : 0.f;
+#pragma unroll
+                  for (int u = 0; u < DS; ++u) {
+                    const float w = t[i][u];
+                    if (GRAD) word_sum[0][b][u] = __builtin_fmaf(p2, w, word_sum[0][b][u]);
+                    word_sum[SETS - 1][b][u] = __builtin_fmaf(p, w, word_sum[SETS - 1][b][u]);
+                  }
+                }
+              }
+            }
+          } else {
           for (int mc = 0; mc < L.mc; ++mc) {
             const int m = mc * 64 + hm;
             if (m >= L.mh) break;
@@ -487,6 +560,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
               }
             }
           }
+          }
         }
       }
     }
@@ -498,6 +572,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
         a[SETS - 1][b] = lds[L.cacc + ((SETS - 1) * QB + b) * nout + t];
         if (GRAD) a[0][b] = lds[L.cacc + b * nout + t];
       }
+#pragma unroll 4
       for (int s = 0; s < nseg; ++s) {
         const float c = A.centroids[(int64_t)segs[s].list * d + hd0 + t];
 #pragma unroll
@@ -516,7 +591,14 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   }
   // the wavefronts' and row groups' histograms become one: H[set][b][m][c], over the first of them
   __syncthreads();
-  float* H = lds + L.hist;
+  float* H = lds + (DS > 0 ? L.score : L.hist);
+  if (DS > 0) {                                // (over the weights: [set][query][wavefront][lane][DS])
+#pragma unroll
+    for (int sb = 0; sb < SETS * QB; ++sb)
+#pragma unroll
+      for (int u = 0; u < (DS > 0 ? DS : 1); ++u)
+        H[((sb * kWaves + wave) * 64 + lane) * DS + u] = hist_lane ? word_sum[sb / QB][sb % QB][u] : 0.f;
+  } else
   for (int i = threadIdx.x; i < SETS * QB * L.mh * 16; i += 256) {
     const int c = i & 15, m = (i >> 4) % L.mh, sb = (i >> 4) / L.mh;
     const int mc = m >> 6, l0 = L.mh < 64 ? m : m & 63;
@@ -546,11 +628,16 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
     }
     for (int i = threadIdx.x; i < SETS * nout; i += 256) {
       const int set = i / nout, t = i - set * nout, m = t / dsub, u = t - m * dsub;
-      const float* cb = A.codebooks + (int64_t)(h0 + m) * 16 * dsub + u;
-      const float* h = H + ((set * QB + b) * L.mc + (m >> 6)) * 1024 + (L.mh < 64 ? m : m & 63);
       float v = lds[L.cacc + (set * QB + b) * nout + t];
+      if (DS > 0) {
+        for (int w = 0; w < kWaves; ++w)
+          for (int r = 0; r < rstep; ++r) v += H[(((set * QB + b) * kWaves + w) * 64 + r * L.mh + m) * DS + u];
+      } else {
+        const float* cb = A.codebooks + (int64_t)(h0 + m) * 16 * dsub + u;
+        const float* h = H + ((set * QB + b) * L.mc + (m >> 6)) * 1024 + (L.mh < 64 ? m : m & 63);
 #pragma unroll
-      for (int c = 0; c < 16; ++c) v = __builtin_fmaf(h[c * 64], cb[c * dsub], v);
+        for (int c = 0; c < 16; ++c) v = __builtin_fmaf(h[c * 64], cb[c * dsub], v);
+      }
       out[(GRAD ? 3 : 2) + i] = v;
     }
   }
@@ -1277,8 +1364,20 @@ void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* p
     else TILES_W(4);
 #undef TILES_W
 #undef TILES
-  } else if (grad) { if (p.qb == 2) run(attend_scan_kernel<2, true>); else run(attend_scan_kernel<1, true>); }
-  else { if (p.qb == 2) run(attend_scan_kernel<2, false>); else run(attend_scan_kernel<1, false>); }
+  } else {
+#define SCAN(DS)                                                                                                \
+  do {                                                                                                          \
+    if (grad) { if (p.qb == 2) run(attend_scan_kernel<2, true, DS>); else run(attend_scan_kernel<1, true, DS>); } \
+    else { if (p.qb == 2) run(attend_scan_kernel<2, false, DS>); else run(attend_scan_kernel<1, false, DS>); }    \
+  } while (0)
+    switch (scan_words(s.g, c.dk, c.v0, grad)) {
+      case 4: SCAN(4); break;
+      case 2: SCAN(2); break;
+      case 1: SCAN(1); break;
+      default: SCAN(0);
+    }
+#undef SCAN
+  }
   const dim3 gj((unsigned)c.nq, (unsigned)((p.nout + 63) / 64));
   if (grad) attend_join_kernel<true><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, c.g_lse, c.scale, c.dtype, c.out, nullptr);
   else attend_join_kernel<false><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, nullptr, c.scale, c.dtype, c.out, c.out_lse);
