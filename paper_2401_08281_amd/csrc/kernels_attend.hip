@@ -17,6 +17,7 @@
 
 namespace {
 
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kRound = 2048;        // rows of a round
 constexpr int kSegments = 64;       // lists it may span
@@ -63,7 +64,8 @@ struct ScanArgs {
   int64_t ld;
 };
 
-struct Segment { int64_t pos; int32_t list, first, len, tile; };   // rows [first, first + len) of a round, its first run
+// Rows [first, first + len) of a round; first is a multiple of eight, and weights up to the next one are zero.
+struct Segment { int64_t pos; int32_t list, first, len, pad; };
 struct Tile { int64_t pos; int32_t first, len_seg; };              // a run: length, segment << 8
 
 // The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
@@ -181,6 +183,16 @@ __device__ __forceinline__ void score_row(const uint8_t* row, const u32 (&words)
   for (int b = 0; b < QB; ++b) out[b] = (acc[0][b] + acc[1][b]) + bias[b];
 }
 
+// N weights of consecutive rows (a multiple of 16 bytes from a multiple of 16 bytes on)
+template <int N>
+__device__ __forceinline__ void load_weights(const float* p, float (&w)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p + i);
+    w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+  }
+}
+
 // Two rows' weights into one column of a histogram: both cells are read before either is written; where the codes are
 // equal both writes carry the sum.
 __device__ __forceinline__ void add_pair(float* h, u32 c0, u32 c1, float p0, float p1) {
@@ -291,14 +303,15 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       }
       const int64_t have = e > b ? e - b : 0;
       const int len0 = (int)(have < kRound ? have : kRound);
-      int end = len0;                             // inclusive prefix sum
+      int end = (len0 + 7) & ~7;                  // inclusive prefix sum
+      const int len8 = end;
 #pragma unroll
       for (int w = 1; w < 64; w <<= 1) {
         const int o = __shfl_up(end, w);
         if (lane >= w) end += o;
       }
-      const int first = end - len0;
-      const int len = first >= kRound ? 0 : (end > kRound ? kRound - first : len0);
+      const int first = end - len8;
+      const int len = first >= kRound ? 0 : (len0 < kRound - first ? len0 : kRound - first);
       const u64 taken = __ballot(len > 0);
       int runs = (len + 63) / 64, run_end = runs;
 #pragma unroll
@@ -308,7 +321,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       }
       if (len > 0) {
         const int at = __popcll(taken & ((1ull << lane) - 1));
-        segs[at] = Segment{b, list, first, len, run_end - runs};
+        segs[at] = Segment{b, list, first, len, 0};
         for (int i = 0; i < runs; ++i)
           tiles[run_end - runs + i] = Tile{b + i * 64, first + i * 64, (len - i * 64 < 64 ? len - i * 64 : 64) | at << 8};
       }
@@ -318,7 +331,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       const int stop = open ? __ffsll(open) - 1 : 64;
       if (lane == (stop < 64 ? stop : 63)) {
         ctl[0] = __popcll(taken);
-        ctl[1] = first + len < kRound ? first + len : kRound;
+        ctl[1] = end < kRound ? end : kRound;
         ctl[2] = next + stop;
         *offset = stop < 64 ? (stop == 0 ? off + len : len) : 0;
       }
@@ -379,7 +392,15 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
       for (int w = 0; w < kRowWords; ++w) now[w] = words[w];
       const int64_t my_id = id;
       if (ti + kWaves < ntile) fetch(ti + kWaves);
-      if (lane < (tl.len_seg & 255)) {
+      const int n = tl.len_seg & 255;
+      if (lane >= n && lane < ((n + 7) & ~7)) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+          lds[L.score + i * QB + b] = GRAD ? 0.f : neg_inf();
+          if (GRAD) lds[L.score2 + i * QB + b] = 0.f;
+        }
+      }
+      if (lane < n) {
         float acc[QB], acc2[QB];
         const uint8_t* row = A.codes + (tl.pos + lane) * cs;
         score_row<QB>(row, now, cs, 0, mk, lds + L.lut, lds + L.bias + s * QB, acc);
@@ -505,35 +526,33 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
         if (hist_lane) {
           const float* pr = lds + L.score + tl.first * QB;
           const float* pr2 = lds + L.score2 + tl.first * QB;
-          const int per = 64 / rstep, j0 = rs * per, j1 = n < j0 + per ? n : j0 + per;
+          const int per = 64 / rstep, j0 = rs * per, n8 = (n + 7) & ~7, j1 = n8 < j0 + per ? n8 : j0 + per;
           if constexpr (DS > 0) {
             typedef float words_t __attribute__((ext_vector_type(DS)));
             const uint8_t* cb = ct + (h0 + hm) / 2 * kCodeRun;
             const int sh = ((h0 + hm) & 1) * 4;
             const float* tab = lds + L.words + hm * DS;
+            const u32 stride = L.mh * DS;
             for (int j = j0; j < j1; j += 8) {
-              u64 c8;
-              __builtin_memcpy(&c8, __builtin_assume_aligned(cb + j, 8), 8);
+              u32x2 c8 = *reinterpret_cast<const u32x2*>(cb + j);
               c8 >>= sh;
               words_t t[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i)
-                t[i] = *reinterpret_cast<const words_t*>(tab + ((u32)(c8 >> (8 * i)) & 15u) * (L.mh * DS));
+                t[i] = *reinterpret_cast<const words_t*>(tab + __umul24((c8[i >> 2] >> (8 * (i & 3))) & 15u, stride));
+              float p[8 * QB], p2[8 * QB];
+              load_weights<8 * QB>(pr + j * QB, p);
+              if (GRAD) load_weights<8 * QB>(pr2 + j * QB, p2);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const bool in = j + i < j1;              // (rows past the end: nothing, wherever their codes point)
-                const int at = (in ? j + i : j0) * QB;
+              for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int b = 0; b < QB; ++b) {
-                  const float p = in ? pr[at + b] : 0.f, p2 = GRAD && in ? pr2[at + b] : 0.f;
+                for (int b = 0; b < QB; ++b)
 #pragma unroll
                   for (int u = 0; u < DS; ++u) {
                     const float w = t[i][u];
-                    if (GRAD) word_sum[0][b][u] = __builtin_fmaf(p2, w, word_sum[0][b][u]);
-                    word_sum[SETS - 1][b][u] = __builtin_fmaf(p, w, word_sum[SETS - 1][b][u]);
+                    if (GRAD) word_sum[0][b][u] = __builtin_fmaf(p2[i * QB + b], w, word_sum[0][b][u]);
+                    word_sum[SETS - 1][b][u] = __builtin_fmaf(p[i * QB + b], w, word_sum[SETS - 1][b][u]);
                   }
-                }
-              }
             }
           } else {
           for (int mc = 0; mc < L.mc; ++mc) {
@@ -543,19 +562,18 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
             const int sh = ((h0 + m) & 1) * 4;
             float* hc = hist + mc * 1024 + lane;
             for (int j = j0; j < j1; j += 8) {
-              u64 c8;
-              __builtin_memcpy(&c8, __builtin_assume_aligned(cb + j, 8), 8);
+              u32x2 c8 = *reinterpret_cast<const u32x2*>(cb + j);
               c8 >>= sh;
+              float p[8 * QB], p2[8 * QB];
+              load_weights<8 * QB>(pr + j * QB, p);
+              if (GRAD) load_weights<8 * QB>(pr2 + j * QB, p2);
 #pragma unroll
               for (int i = 0; i < 8; i += 2) {
-                const u32 ca = (u32)(c8 >> (8 * i)) & 15u, cc = (u32)(c8 >> (8 * i + 8)) & 15u;
-                // (rows past the end: nothing, wherever their codes point)
-                const bool in0 = j + i < j1, in1 = j + i + 1 < j1;
-                const int at0 = (in0 ? j + i : j0) * QB, at1 = (in1 ? j + i + 1 : j0) * QB;
+                const u32 ca = (c8[i >> 2] >> (8 * (i & 3))) & 15u, cc = (c8[i >> 2] >> (8 * (i & 3) + 8)) & 15u;
 #pragma unroll
                 for (int b = 0; b < QB; ++b) {
-                  if (GRAD) add_pair(hc + b * L.mc * 1024, ca, cc, in0 ? pr2[at0 + b] : 0.f, in1 ? pr2[at1 + b] : 0.f);
-                  add_pair(hc + ((SETS - 1) * QB + b) * L.mc * 1024, ca, cc, in0 ? pr[at0 + b] : 0.f, in1 ? pr[at1 + b] : 0.f);
+                  if (GRAD) add_pair(hc + b * L.mc * 1024, ca, cc, p2[i * QB + b], p2[(i + 1) * QB + b]);
+                  add_pair(hc + ((SETS - 1) * QB + b) * L.mc * 1024, ca, cc, p[i * QB + b], p[(i + 1) * QB + b]);
                 }
               }
             }
@@ -661,7 +679,6 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
 // relative to the centroid part of <g, v> of the present list, which is exchanged when the list changes.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef u32 u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTileRows = 64;
 constexpr int kTableBits = 14;                 // weights are held times 2^14
