@@ -11,6 +11,8 @@
 // column of its wavefront's H only, so additions keep their order and banks never collide.  (Additions by LDS atomics ran
 // at 24 cycles a wavefront, three times the whole scan.)  Partial results of the parts are joined by a second kernel.
 // Bound by LDS: one look-up of QB values, and one of a codeword or a histogram cell, for every code.
+#include <algorithm>
+
 #include "../../include/vs_softmax.h"
 #include "common.hpp"
 #include "softmax.hpp"
@@ -1334,10 +1336,15 @@ AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, i
   p.qb = scan_queries(g, dk, v0, nq, nprobe > 0, grad);
   p.lds = scan_lds(g, dk, v0, p.qb, grad).total * 4;
   p.fits = p.lds <= kMaxLds;
-  // some eight workgroups a CU; parts of 256 rows or one probe at least
-  const int64_t groups = (nq + p.qb - 1) / p.qb, want = groups > 0 ? (2048 + groups - 1) / groups : 1;
-  const int64_t most = nprobe > 0 ? nprobe : (ntotal + 255) / 256;
-  int64_t splits = want < most ? want : most;
+  // Parts of some 2048 rows, as many as make eight workgroups a CU: what a workgroup begins and ends with costs as much as
+  // some 500 rows (333 queries of 3200 rows each: 2 parts 112 us, 3 125 us, 6 143 us; 1000 of 7800: 1 part 711 us, 2
+  // 650 us, 3 618 us).  Few queries are cut finer, down to 256 rows, for two workgroups a CU.
+  const int64_t groups = (nq + p.qb - 1) / p.qb > 0 ? (nq + p.qb - 1) / p.qb : 1;
+  const int64_t rows = nprobe > 0 ? ntotal * nprobe / g.nlist : ntotal;
+  const int64_t long_parts = std::min<int64_t>((2048 + groups - 1) / groups, (rows + 1024) / 2048);
+  const int64_t short_parts = std::min<int64_t>((512 + groups - 1) / groups, (rows + 255) / 256);
+  int64_t splits = long_parts > short_parts ? long_parts : short_parts;
+  if (nprobe > 0 && splits > nprobe) splits = nprobe;
   if (splits < 1) splits = 1;
   if (nprobe > 0) {
     p.per = (nprobe + splits - 1) / splits;
