@@ -701,8 +701,10 @@ __host__ __device__ inline CodeSet code_set(int m0, int n, int dsub, int w) {
 }
 struct TileLds {                               // bytes
   int ktab, gtab, vtab, qf, gf, krow, grow, vcol, p, ids, red, stat, cent, total;
-  int p_stride, p_set;
+  int p_stride, p_set, stage;
 };
+// 64-component runs of the result that a tile kernel is made for
+__host__ __device__ inline int tile_runs(int nout) { return nout <= 64 ? 1 : (nout <= 128 ? 2 : (nout <= 256 ? 4 : 12)); }
 __host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, int w, int nq, int planes, bool grad) {
   TileLds o{};
   int at = 0;
@@ -712,16 +714,18 @@ __host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, 
   const int nout = grad ? dk : dv, mo = grad ? mk : mv;
   o.ktab = take(k.ppc * 4 * k.mq * 16 * k.entry);
   o.gtab = take(grad ? v.ppc * 4 * v.mq * 16 * v.entry : 0);
-  o.vtab = take((nout + 15) / 16 * 16 * 64);
+  o.vtab = take(tile_runs(nout) * 64 * 64);
   o.qf = take(planes * nq * k.steps * 1024);
   o.gf = take(grad ? planes * nq * v.steps * 1024 : 0);
-  o.krow = take(kTileRows * k.stride);
+  o.krow = take(kTileRows * k.stride);           // a stage: rows' codes, their ids; two of them
   o.grow = take(grad ? kTileRows * v.stride : 0);
   o.vcol = take(mo * 72);
+  o.ids = take(kTileRows * 8);
+  o.stage = at - o.krow;
+  at += o.stage;
   o.p_stride = kTileRows * 2 + 16;
   o.p_set = planes * nq * 16 * o.p_stride;
   o.p = take((grad ? 2 : 1) * o.p_set);
-  o.ids = take(kTileRows * 8);
   o.red = take(4 * 2 * nq * 16 * 4);
   o.stat = take(nq * 16 * 6 * 4);
   o.cent = take((dk + dv) * 4);
@@ -761,26 +765,64 @@ __device__ __forceinline__ void build_rows_table(char* tab, const CodeSet& c, co
     }
   }
 }
-// Operand B of a code set: the vectors' components in the order of the lanes' steps, [plane][block of 16][step][64 lanes].
+// A vector's components under a lane group's codes [g mq, (g + 1) mq) of a set, handled by one thread: n of them from t0 on.
+struct Share { int t0, n; };
+__device__ __forceinline__ Share share_of(const CodeSet& c, int g, int dsub) {
+  const int c0 = g * c.mq, c1 = c0 + c.mq < c.n ? c0 + c.mq : c.n;
+  return {c0 * dsub, c1 > c0 ? (c1 - c0) * dsub : 0};
+}
+// f(t, value) for the share's components, eight loads in flight
+template <int DT, typename F>
+__device__ __forceinline__ void each_component(const void* row, const Share& s, F f) {
+  int t = 0;
+  for (; t + 8 <= s.n; t += 8) {
+    float v[8];
+    if (DT == VS_FP32) {
+      __builtin_memcpy(v, static_cast<const float*>(row) + s.t0 + t, 32);
+    } else if (DT == VS_FP16) {
+      _Float16 e[8];
+      __builtin_memcpy(e, static_cast<const _Float16*>(row) + s.t0 + t, 16);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = (float)e[u];
+    } else {
+      __bf16 e[8];
+      __builtin_memcpy(e, static_cast<const __bf16*>(row) + s.t0 + t, 16);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = (float)e[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) f(t + u, v[u]);
+  }
+  for (; t < s.n; ++t) f(t, load_as_f32(row, s.t0 + t, DT));
+}
+template <typename F>
+__device__ __forceinline__ void each_component(const void* row, const Share& s, int dtype, F f) {
+  if (dtype == VS_FP32) each_component<VS_FP32>(row, s, f);
+  else if (dtype == VS_FP16) each_component<VS_FP16>(row, s, f);
+  else each_component<VS_BF16>(row, s, f);
+}
+__device__ __forceinline__ const void* row_of(const void* p, int64_t row, int ld, int dtype) {
+  return static_cast<const char*>(p) + row * ld * (dtype == VS_FP32 ? 4 : 2);
+}
+// Operand B of a code set, [plane][block of 16][step][64 lanes]: the lane of query ql and group g holds its share in the
+// order of the steps, times up.
 template <int W, int PL>
-__device__ __forceinline__ void build_query_fragments(char* out, const CodeSet& c, int nqb, const void* src, int64_t ld,
-                                                      int dtype, int64_t q0, int64_t nq, int dsub, const float* up) {
+__device__ __forceinline__ void put_query_fragments(char* out, const CodeSet& c, int nqb, int ql, int g, const void* row,
+                                                    int dtype, int dsub, float up) {
   constexpr int PER = 8 / W;
-  const int n = nqb * c.steps * 64;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const int l = i & 63, step = (i >> 6) % c.steps, qb = (i >> 6) / c.steps;
-    const int per_j = c.mq / PER, j = step / per_j, s = step - j * per_j, g = l >> 4;
-    const int ql = qb * 16 + (l & 15);
-    const int64_t qi = q0 + ql;
+  const int n = nqb * c.steps * 64, per_j = c.mq / PER;
+  const Share sh = share_of(c, g, dsub);
+  for (int step = 0; step < c.steps; ++step) {
+    const int j = step / per_j, s = step - j * per_j;
     f16x8 hi, lo;
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
-      const int code = g * c.mq + s * PER + t / W, u = j * W + t % W;
-      float v = 0.f;
-      if (qi < nq && code < c.n && u < dsub) v = load_as_f32(src, qi * ld + code * dsub + u, dtype) * up[ql];
+      const int u = j * W + t % W, at = (s * PER + t / W) * dsub + u;
+      const float v = row && u < dsub && at < sh.n ? load_as_f32(row, sh.t0 + at, dtype) * up : 0.f;
       hi[t] = (_Float16)v;
       lo[t] = (_Float16)(v - (float)hi[t]);
     }
+    const int i = ((ql >> 4) * c.steps + step) * 64 + g * 16 + (ql & 15);
     reinterpret_cast<f16x8*>(out)[i] = hi;
     if (PL == 2) reinterpret_cast<f16x8*>(out)[n + i] = lo;
   }
@@ -794,13 +836,13 @@ __device__ __forceinline__ void rows_product(const char* tab, const CodeSet& c, 
   const char* mine = rows + ((threadIdx.x >> 6) * 16 + (lane & 15)) * c.stride + g * c.mq;
   const u32x4* b = reinterpret_cast<const u32x4*>(frag) + lane;
   const int n = NQ * c.steps * 64;
+  const int per_j = c.mq / PER;
   for (int j = 0; j < c.ppc; ++j) {
     const char* t = tab + (j * 4 + g) * c.mq * 16 * c.entry;
-    for (int s = 0; s < c.mq / PER; ++s) {
+    auto look = [&](int s, u32x4& hi, u32x4& lo) {
       u32 bytes;
       if (W == 4) bytes = *reinterpret_cast<const unsigned short*>(mine + s * 2);
       else bytes = *reinterpret_cast<const u32*>(mine + s * 4);
-      u32x4 hi, lo;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const char* e = t + (s * PER + i) * 16 * c.entry + ((bytes >> (8 * i)) & 15u) * c.entry;
@@ -812,7 +854,9 @@ __device__ __forceinline__ void rows_product(const char* tab, const CodeSet& c, 
           hi[i] = v[0]; lo[i] = v[1];
         }
       }
-      const int step = j * (c.mq / PER) + s;
+    };
+    auto multiply = [&](int s, const u32x4& hi, const u32x4& lo) {
+      const int step = j * per_j + s;
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) {
         const u32x4 q = b[(qb * c.steps + step) * 64];
@@ -820,9 +864,23 @@ __device__ __forceinline__ void rows_product(const char* tab, const CodeSet& c, 
         acc[qb] = mma(lo, q, acc[qb]);
         if (PL == 2) acc[qb] = mma(hi, b[n + (qb * c.steps + step) * 64], acc[qb]);
       }
+    };
+    int s = 0;
+    for (; s + 4 <= per_j; s += 4) {              // four steps' look-ups in flight
+      u32x4 hi[4], lo[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) look(s + i, hi[i], lo[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) multiply(s + i, hi[i], lo[i]);
+      settle_products();
+    }
+    for (; s < per_j; ++s) {
+      u32x4 hi, lo;
+      look(s, hi, lo);
+      multiply(s, hi, lo);
+      settle_products();
     }
   }
-  settle_products();
 }
 
 constexpr int SETS_OF(bool grad) { return grad ? 2 : 1; }
@@ -841,7 +899,6 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   const int64_t r0 = split * A.per, r1 = r0 + A.per < A.ntotal ? r0 + A.per : A.ntotal;
   float* red = reinterpret_cast<float*>(ldsb + L.red);
   float* stat = reinterpret_cast<float*>(ldsb + L.stat);     // per query: up, down of q; up, down of g; bound of w; bias
-  int64_t* ids = reinterpret_cast<int64_t*>(ldsb + L.ids);
   float* cent = reinterpret_cast<float*>(ldsb + L.cent);     // centroid of the list: [dk] keys, [dv] values
 
   // scales: of the key and value codewords, and of every query
@@ -857,41 +914,41 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   float k_up, k_down, v_up, v_down;
   unit_scale(km, &k_up, &k_down);
   unit_scale(vm, &v_up, &v_down);
-  for (int ql = wave; ql < QT; ql += 4) {
-    const int64_t qi = q0 + ql;
+  // four threads a query, a lane group's share of the components each
+  const int ql = threadIdx.x >> 2, qg = threadIdx.x & 3;
+  const bool q_thread = ql < QT;
+  const void* q_row = q_thread && q0 + ql < A.nq ? row_of(A.q, q0 + ql, A.dk, A.dtype) : nullptr;
+  const void* g_row = GRAD && q_row ? row_of(A.g_out, q0 + ql, dv, A.dtype) : nullptr;
+  if (q_thread) {
     float mx = 0.f, gx = 0.f, g1 = 0.f;
-    if (qi < A.nq) {
-      for (int t = lane; t < A.dk; t += 64) mx = fmaxf(mx, fabsf(load_as_f32(A.q, qi * A.dk + t, A.dtype)));
-      if (GRAD)
-        for (int t = lane; t < dv; t += 64) {
-          const float v = fabsf(load_as_f32(A.g_out, qi * dv + t, A.dtype));
-          gx = fmaxf(gx, v);
-          g1 += v;
-        }
+    if (q_row) each_component(q_row, share_of(K, qg, dsub), A.dtype, [&](int, float v) { mx = fmaxf(mx, fabsf(v)); });
+    if (g_row) each_component(g_row, share_of(V, qg, dsub), A.dtype, [&](int, float v) { gx = fmaxf(gx, fabsf(v)); g1 += fabsf(v); });
+#pragma unroll
+    for (int w = 1; w < 4; w <<= 1) {
+      mx = fmaxf(mx, __shfl_xor(mx, w));
+      if (GRAD) { gx = fmaxf(gx, __shfl_xor(gx, w)); g1 += __shfl_xor(g1, w); }
     }
-    mx = wave_max(mx);
     float up, down;
     unit_scale(mx, &up, &down);
-    if (lane == 0) { stat[ql] = up; stat[QT + ql] = down; }
+    if (qg == 0) { stat[ql] = up; stat[QT + ql] = down; }
+    put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, up);
     if (GRAD) {
-      gx = wave_max(gx);
-      g1 = wave_sum(g1);
       float gup, gdown, bup, bdown;
       unit_scale(gx, &gup, &gdown);
       unit_scale(g1 * vm, &bup, &bdown);                     // |<g, t>| <= |g|_1 max |t| < 2 bdown
-      if (lane == 0) { stat[2 * QT + ql] = gup; stat[3 * QT + ql] = gdown; stat[4 * QT + ql] = bdown; }
+      if (qg == 0) { stat[2 * QT + ql] = gup; stat[3 * QT + ql] = gdown; stat[4 * QT + ql] = bdown; }
+      put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, gup);
     }
   }
   __syncthreads();
   build_rows_table<W>(ldsb + L.ktab, K, A.codebooks, dsub, k_up);
   if (GRAD) build_rows_table<W>(ldsb + L.gtab, V, A.codebooks, dsub, v_up);
   const float o_up = GRAD ? k_up : v_up, o_down = GRAD ? k_down : v_down;
-  for (int i = threadIdx.x; i < (nout + 15) / 16 * 256; i += 256) {
+  for (int i = threadIdx.x; i < NB * 64 * 16; i += 256) {
     const int t = i >> 4, c = i & 15, m = t / dsub;
     reinterpret_cast<u32*>(ldsb + L.vtab)[i] = t < nout ? pack_parts(A.codebooks[((int64_t)(om0 + m) * 16 + c) * dsub + t - m * dsub] * o_up) : 0u;
   }
-  build_query_fragments<W, PL>(ldsb + L.qf, K, NQ, A.q, A.dk, A.dtype, q0, A.nq, dsub, stat);
-  if (GRAD) build_query_fragments<W, PL>(ldsb + L.gf, V, NQ, A.g_out, dv, A.dtype, q0, A.nq, dsub, stat + 2 * QT);
+  __syncthreads();
 
   int64_t limit[NQ], seen_to = INT64_MIN;
   float fs[NQ], fg[NQ], fw[NQ], lse[NQ], bias[NQ], mx[NQ], lp[NQ], lw[NQ], sum[NQ], sum2[NQ];
@@ -963,17 +1020,14 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     for (int t = threadIdx.x; t < A.dk; t += 256) cent[t] = c[t];
     for (int t = threadIdx.x; t < dv; t += 256) cent[A.dk + t] = c[A.v0 + t];
     __syncthreads();
-    for (int ql = wave; ql < QT; ql += 4) {                  // <q, c>, <g, c> in fp32
-      const int64_t qi = q0 + ql;
+    if (q_thread) {                                          // <q, c>, <g, c> in fp32
       float s = 0.f, s2 = 0.f;
-      if (qi < A.nq) {
-        for (int t = lane; t < A.dk; t += 64) s = __builtin_fmaf(load_as_f32(A.q, qi * A.dk + t, A.dtype), cent[t], s);
-        if (GRAD)
-          for (int t = lane; t < dv; t += 64) s2 = __builtin_fmaf(load_as_f32(A.g_out, qi * dv + t, A.dtype), cent[A.dk + t], s2);
-      }
-      s = wave_sum(s);
-      if (GRAD) s2 = wave_sum(s2);
-      if (lane == 0) { red[ql] = s * A.scale; red[QT + ql] = s2; }
+      const Share ks = share_of(K, qg, dsub), vs = share_of(V, qg, dsub);
+      if (q_row) each_component(q_row, ks, A.dtype, [&](int t, float v) { s = __builtin_fmaf(v, cent[ks.t0 + t], s); });
+      if (g_row) each_component(g_row, vs, A.dtype, [&](int t, float v) { s2 = __builtin_fmaf(v, cent[A.dk + vs.t0 + t], s2); });
+#pragma unroll
+      for (int w = 1; w < 4; w <<= 1) { s += __shfl_xor(s, w); if (GRAD) s2 += __shfl_xor(s2, w); }
+      if (qg == 0) { red[ql] = s * A.scale; red[QT + ql] = s2; }
     }
     __syncthreads();
 #pragma unroll
@@ -1018,61 +1072,74 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       cur_end = A.list_off[cur + 1] < r1 ? A.list_off[cur + 1] : r1;
     }
   };
-  advance();
-  int n = pos < r1 ? (int)(cur_end - pos < kTileRows ? cur_end - pos : kTileRows) : 0;
-  if (n > 0) fetch(pos, n);
-  while (n > 0) {
-    const int here = n, here_list = cur;
-    const int64_t my_id = ahead_id;
-    u32 word[kWords];
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) word[i] = ahead[i];
-    pos += n;
-    advance();
-    n = pos < r1 ? (int)(cur_end - pos < kTileRows ? cur_end - pos : kTileRows) : 0;
-    const bool any = __ballot(lane < here && my_id < seen_to) != 0;   // (the same rows in every wavefront)
-    if (n > 0) fetch(pos, n);
-    if (!any) continue;
-    if (here_list != list) { close_list(); open_list(here_list); }
-    else __syncthreads();                                     // the tile before has been read
-    // codes as bytes: along rows for the scores, along components for the product
+  // The next run that some query sees, its codes in registers: {rows, list}; rows 0 at the end.
+  int next_n = 0, next_list = -1;
+  auto take_next = [&]() {
+    while (true) {
+      advance();
+      next_n = pos < r1 ? (int)(cur_end - pos < kTileRows ? cur_end - pos : kTileRows) : 0;
+      if (next_n == 0) return;
+      next_list = cur;
+      fetch(pos, next_n);
+      pos += next_n;
+      if (!A.limits || __ballot(lane < next_n && ahead_id < seen_to) != 0) return;   // (the same rows in every wavefront)
+    }
+  };
+  // Codes as bytes: along rows for the scores, along components for the product.
+  auto put_stage = [&](int which) {
+    char* st = ldsb + which * L.stage;
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       const int w = wave + 4 * i;
       if (w < words) {
-      const u32 even = word[i] & 0x0F0F0F0Fu, odd = (word[i] >> 4) & 0x0F0F0F0Fu;
-      const u32 b0 = __builtin_amdgcn_perm(odd, even, 0x05010400u), b1 = __builtin_amdgcn_perm(odd, even, 0x07030602u);
-      const int m = w * 8;
-      auto row_bytes = [&](char* rows, const CodeSet& c) {
-        const int at = m - c.m0;
-        char* out = rows + lane * c.stride;
-        if (at >= 0 && at + 8 <= 4 * c.mq && (at & 3) == 0) {
-          *reinterpret_cast<u32*>(out + at) = b0;
-          *reinterpret_cast<u32*>(out + at + 4) = b1;
-        } else {
+        const u32 even = ahead[i] & 0x0F0F0F0Fu, odd = (ahead[i] >> 4) & 0x0F0F0F0Fu;
+        const u32 b0 = __builtin_amdgcn_perm(odd, even, 0x05010400u), b1 = __builtin_amdgcn_perm(odd, even, 0x07030602u);
+        const int m = w * 8;
+        auto row_bytes = [&](char* rows, const CodeSet& c) {
+          const int at = m - c.m0;
+          char* out = rows + lane * c.stride;
+          if (at >= 0 && at + 8 <= 4 * c.mq && (at & 3) == 0) {
+            *reinterpret_cast<u32*>(out + at) = b0;
+            *reinterpret_cast<u32*>(out + at + 4) = b1;
+          } else {
 #pragma unroll
-          for (int u = 0; u < 8; ++u)
-            if (at + u >= 0 && at + u < 4 * c.mq) out[at + u] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
-        }
-      };
-      row_bytes(ldsb + L.krow, K);
-      if (GRAD) row_bytes(ldsb + L.grow, V);
+            for (int u = 0; u < 8; ++u)
+              if (at + u >= 0 && at + u < 4 * c.mq) out[at + u] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+          }
+        };
+        row_bytes(st + L.krow, K);
+        if (GRAD) row_bytes(st + L.grow, V);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (m + u >= om0 && m + u < om0 + mo) (ldsb + L.vcol)[(m + u - om0) * 72 + lane] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+        for (int u = 0; u < 8; ++u)
+          if (m + u >= om0 && m + u < om0 + mo) (st + L.vcol)[(m + u - om0) * 72 + lane] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
       }
     }
-    if (wave == 0) ids[lane] = my_id;
-    __syncthreads();
+    if (wave == 0 && A.limits) reinterpret_cast<int64_t*>(st + L.ids)[lane] = ahead_id;
+  };
+
+  take_next();
+  int here = next_n, here_list = next_list, turn = 0;
+  if (here > 0) {
+    put_stage(0);
+    take_next();
+  }
+  __syncthreads();
+  // A stage is written while the one before it is multiplied: two barriers a tile, after the maxima and after the weights.
+  while (here > 0) {
+    if (here_list != list) { close_list(); open_list(here_list); }
+    char* st = ldsb + (turn & 1) * L.stage;
+    const int64_t* ids = reinterpret_cast<const int64_t*>(st + L.ids);
     f32x4 s[NQ] = {}, t[NQ] = {};
-    rows_product<W, NQ, PL>(ldsb + L.ktab, K, ldsb + L.krow, ldsb + L.qf, s);
-    if (GRAD) rows_product<W, NQ, PL>(ldsb + L.gtab, V, ldsb + L.grow, ldsb + L.gf, t);
+    rows_product<W, NQ, PL>(ldsb + L.ktab, K, st + L.krow, ldsb + L.qf, s);
+    if (GRAD) rows_product<W, NQ, PL>(ldsb + L.gtab, V, st + L.grow, ldsb + L.gf, t);
     const int row = wave * 16 + 4 * g;
     bool row_in[4];
     int64_t row_id[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) { row_in[r] = row + r < here; row_id[r] = ids[row + r]; }
-    if (!GRAD) {
+    for (int r = 0; r < 4; ++r) { row_in[r] = row + r < here; row_id[r] = A.limits ? ids[row + r] : 0; }
+    if (GRAD) {
+      __syncthreads();                                        // the weights of the tile before have been multiplied
+    } else {
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) {
         float m = neg_inf();
@@ -1136,6 +1203,13 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
         if (PL == 2) *reinterpret_cast<u32x2*>(out + QT * L.p_stride) = u32x2{wl[0], wl[1]};
       }
     }
+    here = next_n;
+    here_list = next_list;
+    ++turn;
+    if (here > 0) {
+      put_stage(turn & 1);
+      take_next();
+    }
     __syncthreads();
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
@@ -1150,8 +1224,8 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const int t0 = (nb * 4 + wave) * 16;
-        if (t0 < nout) {
-        const u32x2 c8 = *reinterpret_cast<const u32x2*>(ldsb + L.vcol + vdim[nb] + ks * 32 + g * 8);
+        if (NB <= 4 || t0 < nout) {                             // (tables reach over NB 64 components)
+        const u32x2 c8 = *reinterpret_cast<const u32x2*>(st + L.vcol + vdim[nb] + ks * 32 + g * 8);
         const char* tab = ldsb + L.vtab + (t0 + col) * 64;
         u32 e[8];
 #pragma unroll
@@ -1306,7 +1380,7 @@ void tiles_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, 
   const int nout = grad ? dk : g.d - v0, planes = dtype == VS_FP32 ? 2 : 1;
   if (nout > 768) return;
   p->w = g.dsub <= 2 ? 2 : 4;
-  p->nb = nout <= 128 ? 2 : (nout <= 256 ? 4 : 12);
+  p->nb = tile_runs(nout);
   p->nq16 = nq > 16 && p->nb <= 4 ? (grad ? 2 : 4) : 1;   // (what a wavefront's registers hold)
   p->lds = tile_lds(g, dk, v0, p->w, p->nq16, planes, grad).total;
   if (p->nq16 > 1 && p->lds > kMaxLds) { p->nq16 = 1; p->lds = tile_lds(g, dk, v0, p->w, 1, planes, grad).total; }
@@ -1379,7 +1453,8 @@ void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* p
   } while (0)
 #define TILES_W(W)                                                              \
   do {                                                                          \
-    if (p.nq16 > 1) { if (p.nb == 2) TILES(W, 4, 2); else TILES(W, 4, 4); }     \
+    if (p.nq16 > 1) { if (p.nb == 1) TILES(W, 4, 1); else if (p.nb == 2) TILES(W, 4, 2); else TILES(W, 4, 4); } \
+    else if (p.nb == 1) TILES(W, 1, 1);                                          \
     else if (p.nb == 2) TILES(W, 1, 2);                                          \
     else if (p.nb == 4) TILES(W, 1, 4);                                          \
     else TILES(W, 1, 12);                                                        \
