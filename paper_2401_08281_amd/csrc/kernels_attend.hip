@@ -20,12 +20,14 @@
 namespace {
 
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kRound = 2048;        // rows of a round
 constexpr int kSegments = 64;       // lists it may span
 constexpr int kTiles = kRound / 64 + kSegments;   // runs of up to 64 rows of one list
 constexpr int kWaves = 4;
 constexpr int kCodeRun = 72;        // bytes of a staged run of 64 rows' codes (18 words: runs start in different banks)
+// (the same in all lanes, and known to be: what follows from it is scalar)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
 __device__ __forceinline__ float wave_sum(float v) {
@@ -209,7 +211,7 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   extern __shared__ __align__(16) float lds[];
   const ScanLds L = scan_lds(A.g, A.dk, A.v0, QB, GRAD);
   constexpr int SETS = GRAD ? 2 : 1;
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int lane = lane_id(), wave = wave_id();
   const int d = A.g.d, dsub = A.g.dsub, M = A.g.M, cs = A.g.code_size, dv = d - A.v0;
   const int mk = A.dk / dsub, mv = dv / dsub, mv0 = M - mv;
   const int h0 = GRAD ? 0 : mv0, hd0 = GRAD ? 0 : A.v0, nout = GRAD ? A.dk : dv;   // the histogrammed sub-quantizers
@@ -744,6 +746,17 @@ __device__ __forceinline__ u32 pack_parts(float v) {     // {head, tail}
   const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
   return (u32)__builtin_bit_cast(unsigned short, hi) | (u32)__builtin_bit_cast(unsigned short, lo) << 16;
 }
+// Four numbers as heads and tails, two to a word
+__device__ __forceinline__ void pack_4(const float (&v)[4], u32 (&hi)[2], u32 (&lo)[2]) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f16x2 h = {(_Float16)v[2 * i], (_Float16)v[2 * i + 1]};
+    const f16x2 l = {(_Float16)(v[2 * i] - (float)h[0]), (_Float16)(v[2 * i + 1] - (float)h[1])};
+    hi[i] = __builtin_bit_cast(u32, h);
+    lo[i] = __builtin_bit_cast(u32, l);
+  }
+}
 __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
@@ -833,7 +846,7 @@ template <int W, int NQ, int PL>
 __device__ __forceinline__ void rows_product(const char* tab, const CodeSet& c, const char* rows, const char* frag, f32x4 (&acc)[NQ]) {
   constexpr int PER = 8 / W;
   const int lane = lane_id(), g = lane >> 4;
-  const char* mine = rows + ((threadIdx.x >> 6) * 16 + (lane & 15)) * c.stride + g * c.mq;
+  const char* mine = rows + (wave_id() * 16 + (lane & 15)) * c.stride + g * c.mq;
   const u32x4* b = reinterpret_cast<const u32x4*>(frag) + lane;
   const int n = NQ * c.steps * 64;
   const int per_j = c.mq / PER;
@@ -889,7 +902,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   extern __shared__ __align__(16) char ldsb[];
   const TileLds L = tile_lds(A.g, A.dk, A.v0, W, NQ, PL, GRAD);
   constexpr int QT = NQ * 16, SETS = GRAD ? 2 : 1;
-  const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
+  const int lane = lane_id(), wave = wave_id(), g = lane >> 4, col = lane & 15;
   const int d = A.g.d, dsub = A.g.dsub, M = A.g.M, cs = A.g.code_size, dv = d - A.v0;
   const int mk = A.dk / dsub, mv = dv / dsub, mv0 = M - mv;
   const CodeSet K = code_set(0, mk, dsub, W), V = code_set(mv0, mv, dsub, W);
@@ -951,6 +964,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   __syncthreads();
 
   int64_t limit[NQ], seen_to = INT64_MIN;
+  bool all_in = true;                                        // no query that sees nothing (past the last one, say)
   float fs[NQ], fg[NQ], fw[NQ], lse[NQ], bias[NQ], mx[NQ], lp[NQ], lw[NQ], sum[NQ], sum2[NQ];
   f32x4 o[SETS][NB][NQ] = {};
 #pragma unroll
@@ -958,9 +972,10 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     const int64_t qi = q0 + qb * 16 + col;
     const bool in = qi < A.nq;
     limit[qb] = !in ? INT64_MIN : (A.limits ? A.limits[qi] : INT64_MAX);
-    lse[qb] = GRAD && in ? A.lse[qi] : 0.f;
+    lse[qb] = GRAD && in ? A.lse[qi] * kLog2e : 0.f;
     if (GRAD && lse[qb] == neg_inf()) limit[qb] = INT64_MIN;
-    fs[qb] = A.scale * (k_down * stat[QT + qb * 16 + col]);
+    all_in = all_in && limit[qb] != INT64_MIN;
+    fs[qb] = A.scale * (k_down * stat[QT + qb * 16 + col]) * kLog2e;     // (scores in units of log 2 inside)
     fg[qb] = GRAD ? v_down * stat[3 * QT + qb * 16 + col] : 0.f;
     fw[qb] = GRAD ? 1.f / stat[4 * QT + qb * 16 + col] : 0.f;
     mx[qb] = neg_inf(); lp[qb] = 0.f; lw[qb] = 0.f; sum[qb] = 0.f; sum2[qb] = 0.f; bias[qb] = 0.f;
@@ -998,10 +1013,9 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       float p = 0.f, w = 0.f;
 #pragma unroll
       for (int v = 0; v < 4; ++v) { p += red[(v * 2) * QT + qb * 16 + col]; if (GRAD) w += red[(v * 2 + 1) * QT + qb * 16 + col]; }
-      sum[qb] += p;
+      sum[qb] += p;                              // (sums times 2^14; o also times o_up, and w over its bound)
       sum2[qb] += w;
-      // o is held times 2^14 / o_down (w also over its bound)
-      const float ps = p * o_up * (float)(1 << kTableBits), ws = GRAD ? w * fw[qb] * o_up * (float)(1 << kTableBits) : 0.f;
+      const float ps = p * o_up, ws = GRAD ? w * fw[qb] * o_up : 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -1027,7 +1041,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       if (g_row) each_component(g_row, vs, A.dtype, [&](int t, float v) { s2 = __builtin_fmaf(v, cent[A.dk + vs.t0 + t], s2); });
 #pragma unroll
       for (int w = 1; w < 4; w <<= 1) { s += __shfl_xor(s, w); if (GRAD) s2 += __shfl_xor(s2, w); }
-      if (qg == 0) { red[ql] = s * A.scale; red[QT + ql] = s2; }
+      if (qg == 0) { red[ql] = s * A.scale * kLog2e; red[QT + ql] = s2; }
     }
     __syncthreads();
 #pragma unroll
@@ -1133,12 +1147,23 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     rows_product<W, NQ, PL>(ldsb + L.ktab, K, st + L.krow, ldsb + L.qf, s);
     if (GRAD) rows_product<W, NQ, PL>(ldsb + L.gtab, V, st + L.grow, ldsb + L.gf, t);
     const int row = wave * 16 + 4 * g;
-    bool row_in[4];
-    int64_t row_id[4];
+    // which of the 4 x NQ pairs count: all of a whole run that every query sees to its end
+    u32 sees = ~0u;
+    if (here < kTileRows || A.limits || !all_in) {
+      sees = 0;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) { row_in[r] = row + r < here; row_id[r] = A.limits ? ids[row + r] : 0; }
+      for (int r = 0; r < 4; ++r) {
+        const int64_t id = A.limits ? ids[row + r] : 0;
+#pragma unroll
+        for (int qb = 0; qb < NQ; ++qb) sees |= (u32)(row + r < here && id < limit[qb]) << (qb * 4 + r);
+      }
+    }
     if (GRAD) {
       __syncthreads();                                        // the weights of the tile before have been multiplied
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[qb][r] = __builtin_fmaf(s[qb][r], fs[qb], bias[qb]);
     } else {
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) {
@@ -1146,7 +1171,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float v = __builtin_fmaf(s[qb][r], fs[qb], bias[qb]);
-          s[qb][r] = row_in[r] && row_id[r] < limit[qb] ? v : neg_inf();
+          s[qb][r] = (sees >> (qb * 4 + r)) & 1u ? v : neg_inf();
           m = fmaxf(m, s[qb][r]);
         }
         m = fmaxf(m, __shfl_xor(m, 16));
@@ -1159,8 +1184,8 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
         float m = mx[qb];
 #pragma unroll
         for (int v = 0; v < 4; ++v) m = fmaxf(m, red[v * QT + qb * 16 + col]);
-        if (m > mx[qb]) {
-          const float f = mx[qb] == neg_inf() ? 1.f : exp_neg(mx[qb] - m);      // (nothing yet: zeros to scale)
+        if (__ballot(m > mx[qb]) != 0) {
+          const float f = mx[qb] == neg_inf() ? 1.f : __builtin_amdgcn_exp2f(mx[qb] - m);      // (nothing yet: zeros to scale)
           lp[qb] *= f;
           sum[qb] *= f;
 #pragma unroll
@@ -1171,29 +1196,25 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     }
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) {
-      const float base = GRAD ? lse[qb] : (mx[qb] > neg_inf() ? mx[qb] : 0.f);
-      u32 ph[2], pl[2], wh[2], wl[2];
+      // weights times 2^14 throughout
+      const float base = (GRAD ? lse[qb] : (mx[qb] > neg_inf() ? mx[qb] : 0.f)) - (float)kTableBits;
+      float p[4], w[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float p, w = 0.f;
+        p[r] = __builtin_amdgcn_exp2f(s[qb][r] - base);
+        w[r] = 0.f;
         if (GRAD) {
-          const bool sees = row_in[r] && row_id[r] < limit[qb];
-          p = sees ? exp_neg(__builtin_fmaf(s[qb][r], fs[qb], bias[qb]) - base) : 0.f;
-          w = sees ? p * (t[qb][r] * fg[qb]) : 0.f;
-          lw[qb] += w;
-        } else {
-          p = exp_neg(s[qb][r] - base);
+          if (!((sees >> (qb * 4 + r)) & 1u)) p[r] = 0.f;
+          w[r] = p[r] * (t[qb][r] * fg[qb]);
+          if (!((sees >> (qb * 4 + r)) & 1u)) w[r] = 0.f;
+          lw[qb] += w[r];
+          w[r] *= fw[qb];
         }
-        lp[qb] += p;
-        const u32 pp = pack_parts(p * (float)(1 << kTableBits)), pw = GRAD ? pack_parts(w * fw[qb] * (float)(1 << kTableBits)) : 0u;
-        if (r & 1) {
-          ph[r >> 1] |= pp << 16; pl[r >> 1] |= pp & 0xFFFF0000u;
-          wh[r >> 1] |= pw << 16; wl[r >> 1] |= pw & 0xFFFF0000u;
-        } else {
-          ph[r >> 1] = pp & 0xFFFFu; pl[r >> 1] = pp >> 16;
-          wh[r >> 1] = pw & 0xFFFFu; wl[r >> 1] = pw >> 16;
-        }
+        lp[qb] += p[r];
       }
+      u32 ph[2], pl[2], wh[2], wl[2];
+      pack_4(p, ph, pl);
+      if (GRAD) pack_4(w, wh, wl);
       char* out = ldsb + L.p + (SETS - 1) * L.p_set + (qb * 16 + col) * L.p_stride + row * 2;
       *reinterpret_cast<u32x2*>(out) = u32x2{ph[0], ph[1]};
       if (PL == 2) *reinterpret_cast<u32x2*>(out + QT * L.p_stride) = u32x2{pl[0], pl[1]};
@@ -1260,8 +1281,9 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     float* out = A.part + (qi * A.nsplit + split) * A.ld;
     const float f = o_down * (1.f / (float)(1 << kTableBits));
     if (wave == 0 && g == 0) {
-      out[0] = GRAD ? sum2[qb] : mx[qb];
-      out[1] = sum[qb];
+      constexpr float one = 1.f / (float)(1 << kTableBits);
+      out[0] = GRAD ? sum2[qb] * one : mx[qb] * kLn2;
+      out[1] = sum[qb] * one;
       if (GRAD) out[2] = gbias[qb];
     }
 #pragma unroll
@@ -1291,7 +1313,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
   __shared__ float red[8];
   __shared__ float sums[4][64];
   const int64_t qi = blockIdx.x;
-  const int lane = lane_id(), wave = threadIdx.x >> 6, t = blockIdx.y * 64 + lane;
+  const int lane = lane_id(), wave = wave_id(), t = blockIdx.y * 64 + lane;
   const float* p = part + qi * nsplit * ld;
   float inv = 1.f;
   if (!GRAD) {

@@ -18,6 +18,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// (the same in all lanes, and known to be: what follows from it is scalar)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 // e^t for t <= 0 (v_exp_f32: one unit in the last place, results below 2^-126 flush to 0 or a denormal, both fine here)
 __device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
@@ -80,7 +82,7 @@ struct TileMul {
   // acc[ib][jb] of this wavefront: rows 32 (IB wa + ib) .., queries 32 (JB wb + jb) ..; K units [ku0, ku1), at least one
   static __device__ __forceinline__ void run(const SmMatrix& A, int64_t a0, const SmMatrix& B, int64_t b0, int64_t ku0,
                                              int64_t ku1, char* lds, f32x16 (&acc)[IB][JB]) {
-    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int lane = lane_id(), wave = wave_id();
     const int wa = wave & 1, wb = wave >> 1;
     // rows past the last one repeat it: their results are dropped
     const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
@@ -193,7 +195,7 @@ __device__ __forceinline__ Best join_mixed(Best a, Best b) {
 // rowdata: LDS, {row factor, bias} of the workgroup's 256 rows, filled here.
 template <int IB, int JB>
 __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[IB][JB]) {
-  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1;
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1;
   const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + 64 * IB <= S.nx;   // (the same in the workgroup)
   if (!plain) {
     const int64_t j = a0 + threadIdx.x;
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords
   f32x16 acc[4][2] = {};
   TileMul<PLANES, BF16>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
   finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
-  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
   for (int jb = 0; jb < 2; ++jb) {
     const int64_t qi = b0 + wb * 64 + jb * 32 + (lane & 31);
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(256) void sm_scores_few_kernel(const typename Elem<
   constexpr int CH = few_chunk<DT, NT>();
   extern __shared__ __align__(16) char lds[];
   u32x4* frag = reinterpret_cast<u32x4*>(lds);        // [step][NT][64]
-  const int lane = lane_id(), wave = threadIdx.x >> 6, g = lane >> 4;
+  const int lane = lane_id(), wave = wave_id(), g = lane >> 4;
   const int64_t part = blockIdx.x, j0 = part * kSmRecRows + wave * 32;
   const typename F::T* row[2];
 #pragma unroll
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
   __shared__ u64 shared_bound;
   __shared__ float red[3][4];
   const int64_t qi = blockIdx.x;
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  const int lane = lane_id(), wave = wave_id();
   const float4* rec = R.rec + qi * R.parts;
   const T* x = static_cast<const T*>(F.x);
   const T* q = static_cast<const T*>(F.q) + qi * F.d;
@@ -802,7 +804,7 @@ __global__ __launch_bounds__(256) void sm_colmax_kernel(SmSide side0, SmSide sid
   u32* __restrict__ colmax = S.colmax;
   const int64_t n = S.n;
   __shared__ float part[4][64 * V];
-  const int lane = lane_id(), wave = threadIdx.x >> 6, t = (blockIdx.x * 64 + lane) * V;
+  const int lane = lane_id(), wave = wave_id(), t = (blockIdx.x * 64 + lane) * V;
   const int64_t r0 = (int64_t)(blockIdx.y < blocks0 ? blockIdx.y : blockIdx.y - blocks0) * rows_per;
   const int64_t r1 = r0 + rows_per < n ? r0 + rows_per : n;
   float mx[V] = {};
@@ -913,7 +915,7 @@ __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut
   f32x16 acc[IB][JB] = {};
   TileMul<PLANES, BF16, IB, JB>::run(S.x, a0, S.q, b0, 0, S.kunits, lds, acc);
   finish_scores(S, a0, b0, reinterpret_cast<float2*>(lds), acc);
-  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) {
     const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
@@ -1078,7 +1080,7 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
   tile_of(blockIdx.x - split * tiles, ta, tb, &ia, &ib_);
   const int64_t a0 = ia * kBigTile, b0 = ib_ * kBigTile;
   const int64_t k0 = kblocks * split / splits, k1 = kblocks * (split + 1) / splits;
-  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
   f32x16 acc[4][2] = {};
   const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
   const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
@@ -1191,7 +1193,7 @@ __global__ __launch_bounds__(256, 2) void sm_product_small_kernel(SmMatrix A, Sm
   const int64_t k0 = kunits * split / splits, k1 = kunits * (split + 1) / splits;
   f32x16 acc[IB][JB] = {};
   if (k1 > k0) TileMul<PLANES, false, IB, JB>::run(A, a0, B, b0, k0, k1, lds, acc);
-  const int lane = lane_id(), wave = threadIdx.x >> 6, wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) {
     const int64_t b = b0 + (wb * JB + jb) * 32 + (lane & 31);
