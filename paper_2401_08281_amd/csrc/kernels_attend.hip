@@ -1137,8 +1137,9 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     put_stage(0);
     take_next();
   }
-  __syncthreads();
-  // A stage is written while the one before it is multiplied: two barriers a tile, after the maxima and after the weights.
+  block_sync_lds();
+  // A stage is written while the one before it is multiplied: two barriers a tile, after the maxima and after the weights,
+  // which leave the codes that are on their way alone.
   while (here > 0) {
     if (here_list != list) { close_list(); open_list(here_list); }
     char* st = ldsb + (turn & 1) * L.stage;
@@ -1159,7 +1160,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       }
     }
     if (GRAD) {
-      __syncthreads();                                        // the weights of the tile before have been multiplied
+      block_sync_lds();                                        // the weights of the tile before have been multiplied
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb)
 #pragma unroll
@@ -1178,7 +1179,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
         m = fmaxf(m, __shfl_xor(m, 32));
         if (g == 0) red[wave * QT + qb * 16 + col] = m;
       }
-      __syncthreads();
+      block_sync_lds();
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) {
         float m = mx[qb];
@@ -1231,7 +1232,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       put_stage(turn & 1);
       take_next();
     }
-    __syncthreads();
+    block_sync_lds();
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       u32x4 b[SETS][PL][NQ];
