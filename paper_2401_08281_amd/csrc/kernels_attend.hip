@@ -1066,14 +1066,18 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   u32 ahead[kWords];
   int64_t ahead_id = 0;
   auto fetch = [&](int64_t pos, int n) {
-    const bool in = lane < n;
-    const uint8_t* row = A.codes + (pos + (in ? lane : 0)) * cs;
+    const uint8_t* row = A.codes + (pos + (lane < n ? lane : 0)) * cs;
+    // (a word that the row does not fill is loaded so that it ends with the row, and shifted where it is used: no load
+    // hangs on a condition, so none is waited for)
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
       const int w = wave + 4 * i;
-      ahead[i] = in && w < words ? code_word(row, w, cs) : 0u;
+      if (w < words) {
+        if (cs >= 4) __builtin_memcpy(&ahead[i], row + (4 * w + 4 <= cs ? 4 * w : cs - 4), 4);
+        else ahead[i] = code_word(row, w, cs);
+      }
     }
-    ahead_id = in && A.limits ? A.ids[pos + lane] : 0;
+    if (A.limits) ahead_id = lane < n ? A.ids[pos + lane] : INT64_MAX;
   };
 
   int64_t pos = r0;
@@ -1096,7 +1100,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       next_list = cur;
       fetch(pos, next_n);
       pos += next_n;
-      if (!A.limits || __ballot(lane < next_n && ahead_id < seen_to) != 0) return;   // (the same rows in every wavefront)
+      if (!A.limits || __ballot(ahead_id < seen_to) != 0) return;   // (the same rows in every wavefront)
     }
   };
   // Codes as bytes: along rows for the scores, along components for the product.
@@ -1106,7 +1110,8 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     for (int i = 0; i < kWords; ++i) {
       const int w = wave + 4 * i;
       if (w < words) {
-        const u32 even = ahead[i] & 0x0F0F0F0Fu, odd = (ahead[i] >> 4) & 0x0F0F0F0Fu;
+        const u32 word = ahead[i] >> (cs >= 4 && 4 * w + 4 > cs ? 8 * (4 * w + 4 - cs) : 0);
+        const u32 even = word & 0x0F0F0F0Fu, odd = (word >> 4) & 0x0F0F0F0Fu;
         const u32 b0 = __builtin_amdgcn_perm(odd, even, 0x05010400u), b1 = __builtin_amdgcn_perm(odd, even, 0x07030602u);
         const int m = w * 8;
         auto row_bytes = [&](char* rows, const CodeSet& c) {
@@ -1115,7 +1120,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
           if (at >= 0 && at + 8 <= 4 * c.mq && (at & 3) == 0) {
             *reinterpret_cast<u32*>(out + at) = b0;
             *reinterpret_cast<u32*>(out + at + 4) = b1;
-          } else {
+          } else if (at + 8 > 0 && at < 4 * c.mq) {
 #pragma unroll
             for (int u = 0; u < 8; ++u)
               if (at + u >= 0 && at + u < 4 * c.mq) out[at + u] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
@@ -1123,9 +1128,15 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
         };
         row_bytes(st + L.krow, K);
         if (GRAD) row_bytes(st + L.grow, V);
+        char* cols = st + L.vcol + (m - om0) * 72 + lane;
+        if (m >= om0 && m + 8 <= om0 + mo) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-          if (m + u >= om0 && m + u < om0 + mo) (st + L.vcol)[(m + u - om0) * 72 + lane] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+          for (int u = 0; u < 8; ++u) cols[u * 72] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+        } else {
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (m + u >= om0 && m + u < om0 + mo) cols[u * 72] = (char)((u < 4 ? b0 : b1) >> (8 * (u & 3)));
+        }
       }
     }
     if (wave == 0 && A.limits) reinterpret_cast<int64_t*>(st + L.ids)[lane] = ahead_id;
