@@ -818,27 +818,23 @@ __device__ __forceinline__ const void* row_of(const void* p, int64_t row, int ld
   return static_cast<const char*>(p) + row * ld * (dtype == VS_FP32 ? 4 : 2);
 }
 // Operand B of a code set, [plane][block of 16][step][64 lanes]: the lane of query ql and group g holds its share in the
-// order of the steps, times up.
+// order of the steps, times up.  (The fragments hold zeros before.)
 template <int W, int PL>
 __device__ __forceinline__ void put_query_fragments(char* out, const CodeSet& c, int nqb, int ql, int g, const void* row,
                                                     int dtype, int dsub, float up) {
   constexpr int PER = 8 / W;
-  const int n = nqb * c.steps * 64, per_j = c.mq / PER;
-  const Share sh = share_of(c, g, dsub);
-  for (int step = 0; step < c.steps; ++step) {
-    const int j = step / per_j, s = step - j * per_j;
-    f16x8 hi, lo;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const int u = j * W + t % W, at = (s * PER + t / W) * dsub + u;
-      const float v = row && u < dsub && at < sh.n ? load_as_f32(row, sh.t0 + at, dtype) * up : 0.f;
-      hi[t] = (_Float16)v;
-      lo[t] = (_Float16)(v - (float)hi[t]);
-    }
-    const int i = ((ql >> 4) * c.steps + step) * 64 + g * 16 + (ql & 15);
-    reinterpret_cast<f16x8*>(out)[i] = hi;
-    if (PL == 2) reinterpret_cast<f16x8*>(out)[n + i] = lo;
-  }
+  const int plane = nqb * c.steps * 1024, per_j = c.mq / PER;
+  char* lane_at = out + ((ql >> 4) * c.steps * 64 + g * 16 + (ql & 15)) * 16;
+  int code = 0, u = 0;                         // of the component that comes next
+  each_component(row, share_of(c, g, dsub), dtype, [&](int, float x) {
+    const float v = x * up;
+    const _Float16 hi = (_Float16)v;
+    const int step = u / W * per_j + code / PER, t = code % PER * W + u % W;
+    _Float16* at = reinterpret_cast<_Float16*>(lane_at + step * 1024) + t;
+    at[0] = hi;
+    if (PL == 2) at[plane / 2] = (_Float16)(v - (float)hi);
+    if (++u == dsub) { u = 0; ++code; }
+  });
 }
 
 // acc[qb] += rows (16 of this wavefront) x queries over a code set; acc's lane: query lane & 15, rows 4 (lane >> 4) + r
@@ -916,8 +912,13 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
 
   // scales: of the key and value codewords, and of every query
   float km = 0.f, vm = 0.f;
+#pragma unroll 8
   for (int i = threadIdx.x; i < mk * 16 * dsub; i += 256) km = fmaxf(km, fabsf(A.codebooks[i]));
+#pragma unroll 8
   for (int i = threadIdx.x; i < mv * 16 * dsub; i += 256) vm = fmaxf(vm, fabsf(A.codebooks[(int64_t)mv0 * 16 * dsub + i]));
+  for (int i = threadIdx.x; i < PL * NQ * K.steps * 64; i += 256) reinterpret_cast<u32x4*>(ldsb + L.qf)[i] = u32x4{0, 0, 0, 0};
+  if (GRAD)
+    for (int i = threadIdx.x; i < PL * NQ * V.steps * 64; i += 256) reinterpret_cast<u32x4*>(ldsb + L.gf)[i] = u32x4{0, 0, 0, 0};
   km = wave_max(km);
   vm = wave_max(vm);
   if (lane == 0) { red[wave] = km; red[4 + wave] = vm; }
@@ -944,13 +945,13 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     float up, down;
     unit_scale(mx, &up, &down);
     if (qg == 0) { stat[ql] = up; stat[QT + ql] = down; }
-    put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, up);
+    if (q_row) put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, up);
     if (GRAD) {
       float gup, gdown, bup, bdown;
       unit_scale(gx, &gup, &gdown);
       unit_scale(g1 * vm, &bup, &bdown);                     // |<g, t>| <= |g|_1 max |t| < 2 bdown
       if (qg == 0) { stat[2 * QT + ql] = gup; stat[3 * QT + ql] = gdown; stat[4 * QT + ql] = bdown; }
-      put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, gup);
+      if (g_row) put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, gup);
     }
   }
   __syncthreads();
