@@ -24,7 +24,8 @@ extern "C" {
 #endif
 
 enum { VS_FP32 = 0, VS_FP16 = 1, VS_BF16 = 2 };
-#define VS_MAX_TOP 64 /* largest k of vs_flat_logprob */
+#define VS_MAX_TOP 64     /* largest k of vs_flat_logprob */
+#define VS_MAX_ROW 65536 /* largest d of vs_flat_logprob */
 
 /*
  * Log-probabilities under the softmax of exact inner products:
@@ -42,7 +43,7 @@ enum { VS_FP32 = 0, VS_FP16 = 1, VS_BF16 = 2 };
  * Scores are fp32 sums of products that are exact for fp16 and bf16 rows; fp32 rows go as two fp16 parts
  * each, relative to the largest component of their row, and lose at most 2^-21 |q||x| of a score that way (up to 64
  * queries they are multiplied in fp32).  Order among scores closer than their rounding may differ from the exact one.
- * Errors: null pointers (with nq > 0), d < 1, nb or nq outside [0, 2^31), nt < 0, k outside [0, VS_MAX_TOP], unknown
+ * Errors: null pointers (with nq > 0), d outside [1, VS_MAX_ROW], nb or nq outside [0, 2^31), nt < 0, k outside [0, VS_MAX_TOP], unknown
  * dtype, scale not finite, misaligned vectors or work space, a work space that is too small.  nq = 0 is a no-op.
  */
 VS_API int64_t vs_flat_logprob_workspace_bytes(int64_t nb, int64_t nq, int32_t d, int32_t dtype, int32_t k);
@@ -83,10 +84,13 @@ VS_API int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_
  *   limits   [nq] int64 or NULL: query i sees the vectors whose id is below limits[i] (positions up to its own).
  *   out      [nq, d - v0] of `dtype`, out_lse [nq] fp32 (may be NULL).  A query that sees nothing: zeros and -inf.
  * The index is not written.  With 0 < nprobe < nlist the coarse quantizer uses the index's own work space, as
- * vs_ivfpq_search does: such calls on one index must not overlap in time, and the first of a size allocates.
+ * vs_ivfpq_search does: such calls on one index must not overlap in time, the first of a size allocates, and a stream under
+ * capture is refused (VS_ERR_UNSUPPORTED).
  * Errors: null pointers (with nq > 0), an index with another metric or with 8-bit codes (VS_ERR_UNSUPPORTED), dk or v0
  * outside their range or inside a sub-quantizer, nprobe outside [0, VS_MAX_K], scale not finite, misaligned vectors or work space, a
- * work space that is too small; VS_ERR_UNSUPPORTED where the tables of a query exceed the on-chip memory (M above 512).
+ * work space that is too small, an index of another device than the current one; VS_ERR_UNSUPPORTED where the tables of a
+ * query exceed the on-chip memory: with sub-quantizers of up to 8 components, M <= 256 fits where dk = d and v0 = 0 and
+ * M <= 400 where dk = v0 = d / 2, of the gradient M <= 128 and M <= 256.
  */
 VS_API int64_t vs_ivfpq_attend_workspace_bytes(const vs_ivfpq* ix, int64_t nq, int32_t dk, int32_t v0, int32_t dtype,
                                                int32_t nprobe);

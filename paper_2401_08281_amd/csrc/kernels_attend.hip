@@ -706,7 +706,7 @@ struct TileLds {                               // bytes
   int p_stride, p_set, stage;
 };
 // 64-component runs of the result that a tile kernel is made for
-__host__ __device__ inline int tile_runs(int nout) { return nout <= 64 ? 1 : (nout <= 128 ? 2 : (nout <= 256 ? 4 : 12)); }
+__host__ __device__ inline int tile_runs(int nout) { return nout <= 64 ? 1 : (nout <= 128 ? 2 : (nout <= 256 ? 4 : 8)); }
 __host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, int w, int nq, int planes, bool grad) {
   TileLds o{};
   int at = 0;
@@ -1411,9 +1411,20 @@ constexpr int kMaxLds = 160 * 1024;
 // Which tile kernel serves a call, if any: p->tiles, nq16 (16-query blocks of a tile), nb (64-component runs of the result)
 void tiles_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, int dtype, int nprobe, bool grad, AttendPlan* p) {
   p->tiles = false;
-  if (nprobe > 0 || nq < 2 || ntotal < 64 || g.code_size > 64 || ntotal / g.nlist < 64) return;
   const int nout = grad ? dk : g.d - v0, planes = dtype == VS_FP32 ? 2 : 1;
-  if (nout > 768) return;
+  if (nprobe > 0 || nq < 4 || g.code_size > 64 || nout > 512) return;
+  // Tiles or the scan.  The scan's work is its look-ups, nq ntotal (dk + d - v0) / dsub; a tile reads a code once for 16 or
+  // 64 queries, but assembles operands for as many, begins later, and fills up a list's last 64 rows.  Scan and tiles in us,
+  // fp16, dk = d = 128, M = 32 (millions of look-ups in brackets): 3000 codes, 64 queries (12) 26 and 39, 256 (49) 37 and 39,
+  // 1024 (197) 87 and 42; 20,000, 8 queries (10) 26 and 27, 16 (20) 31 and 27, 64 (82) 47 and 38; 1,500,000, 2 queries (192)
+  // 94 and 163, 4 (384) 148 and 158, 8 (768) 213 and 158; 20,000 in lists of 312, 64 queries (82) 52 and 51, 512 197 and 69;
+  // in lists of 78, 64 queries 65 and 67, 512 252 and 91; in lists of 31, 64 queries 96 and 112, 512 366 and 142.  Results of
+  // more than 256 components go 16 queries at a time: 50,000 codes of d = 320, M = 80, 8 queries (64) 62
+  // and 55, 32 queries 205 and 104; sub-vectors of more than four components, which the scan takes as cheaply as short
+  // ones: d = 384, M = 64, 32 queries (205) 89 and 117, 64 (410) 202 and 153; d = 768, M = 64, 256 queries 561 and 570.
+  const double look_ups = (double)nq * (double)ntotal * (double)((dk + g.d - v0) / g.dsub), run = (double)ntotal / g.nlist;
+  const double least = nout > 256 && g.dsub > 4 ? 256e6 : (nq > 16 || nout > 256 ? 48e6 : 16e6);
+  if (run < 24. || look_ups < least * (1. + 100. / run)) return;
   p->w = g.dsub <= 2 ? 2 : 4;
   p->nb = tile_runs(nout);
   p->nq16 = nq > 16 && p->nb <= 4 ? (grad ? 2 : 4) : 1;   // (what a wavefront's registers hold)
@@ -1423,7 +1434,8 @@ void tiles_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, 
   p->tiles = true;
   p->fits = true;
   p->qb = 16 * p->nq16;
-  const int64_t groups = (nq + p->qb - 1) / p->qb, want = (512 + groups - 1) / groups;
+  // Parts for three workgroups a CU (2048 queries on 16,384 codes: 256 workgroups 175 us, 512 122, 768 118, 1024 140)
+  const int64_t groups = (nq + p->qb - 1) / p->qb, want = (768 + groups - 1) / groups;
   const int64_t most = (ntotal + 255) / 256, splits = want < most ? want : most;
   p->per = ((ntotal + splits - 1) / splits + 63) / 64 * 64;
   p->nsplit = (int)((ntotal + p->per - 1) / p->per);
@@ -1492,7 +1504,7 @@ void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* p
     else if (p.nb == 1) TILES(W, 1, 1);                                          \
     else if (p.nb == 2) TILES(W, 1, 2);                                          \
     else if (p.nb == 4) TILES(W, 1, 4);                                          \
-    else TILES(W, 1, 12);                                                        \
+    else TILES(W, 1, 8);                                                        \
   } while (0)
     if (p.w == 2) TILES_W(2);
     else TILES_W(4);

@@ -1346,9 +1346,14 @@ void launch_sm_coefs(const SmGrads& g, int64_t nq, int64_t nb, float4* coef, flo
   sm_coefs_kernel<<<grid_of(nq, 256), 256, 0, st>>>(g, nq, nb, coef, bound, clear, n_clear);
 }
 
-// Few big tiles leave most CUs without one, and each of them alone with its epilogue: 1024 x 1024 x 96 in fp32 took 40 us
-// on 32 tiles of 256 x 128.
-bool sm_gradients_small(int64_t nx, int64_t nq) { return tiles(nx, kTileA) * tiles(nq, kTileB) < 256; }
+// Tiles of 128 x 64 pairs or of 256 x 128.  A pair's epilogue (its probability, the two G) costs as much as some 400 of
+// its products, and four small workgroups on a CU hide it behind each other's products where two big ones do not; what
+// the big ones save is operand traffic, which counts with one plane and long rows.  Small and big in us: fp32 1024 x 1024
+// x 96 59 and 83, bf16 65,536 x 4096: d = 128 946 and 1031, 384 1488 and 1545, 768 2051 and 2010; fp32 16,384 x 4096 x 768
+// 1398 and 1484; bf16 8192 x 2048 x 768 221 and 217, 4096 x 1024 x 768 (128 big tiles for 256 CUs) 109 and 111.
+bool sm_gradients_small(const SmForm& f, int64_t nx, int64_t nq, int64_t kblocks) {
+  return f.planes == 2 || kblocks < 10 || tiles(nx, kTileA) * tiles(nq, kTileB) < 256;
+}
 
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st) {
   auto run = [&](auto kern, int ib, int jb, int lds) {
@@ -1369,13 +1374,15 @@ void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const 
   }
 }
 
-// Splits of K that give a product some 256 workgroups, eight 128-byte blocks each at least; big: tiles of 256 x 256, where
-// they are a quarter of that or more by themselves (a smaller product waits for its few tiles: 96 x 1024 by 1024 took
-// 20.7 us on 16 big workgroups and 10.6 us on smaller tiles).
+// Splits of K that give a product some 256 workgroups, eight 128-byte blocks each at least.  big: tiles of 256 x 256, where
+// they fill the CUs by themselves or K is long enough to split.  Whole gradients on big and on small tiles in us: bf16
+// 65,536 x 4096 x 768 (768 big tiles for dx, 48 with 1024 blocks of K for dq) 2010 and 2591, 65,536 x 4096 x 128 (256 tiles)
+// 1031 and 1077, fp16 30,011 x 777 x 400 (236) 241 and 275; 30,011 x 777 x 100 (118) 169 and 163, bf16 8192 x 2048 x 768
+// (96, 32 blocks of K) 217 and 201, 4096 x 1024 x 768 (48) 111 and 103.
 SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
   SmProductPlan p;
   const int64_t big = (rows_a + kBigTile - 1) / kBigTile * ((rows_b + kBigTile - 1) / kBigTile);
-  p.big = big >= 48;
+  p.big = big >= 160 || (big >= 48 && kblocks >= 256);
   const int64_t n = p.big ? big : tiles(rows_a, 128) * tiles(rows_b, 64), most = kblocks / (p.big ? 8 : 4);
   int64_t want = p.big ? (256 + n / 2) / n : (512 + n - 1) / n;
   if (want > most) want = most;

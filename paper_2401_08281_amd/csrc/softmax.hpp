@@ -80,7 +80,7 @@ struct SmGOut {
   float* db; int64_t db_ld;         // [query tiles, db_ld] partial column sums, or null
   bool small;                       // tiles of 128 rows by 64 queries (256 by 128)
 };
-bool sm_gradients_small(int64_t nx, int64_t nq);
+bool sm_gradients_small(const SmForm& f, int64_t nx, int64_t nq, int64_t kblocks);
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st);
 // out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over workgroups: part[split][b][ld]
 struct SmProductPlan { bool big; int splits; };

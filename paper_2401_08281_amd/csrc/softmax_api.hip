@@ -53,14 +53,20 @@ struct LogprobPlan {
 LogprobPlan logprob_plan(int64_t nb, int64_t nq, int d, int dtype, int k) {
   LogprobPlan p{};
   p.f = form_of(dtype);
-  p.few = nq <= kSmFewQueries;
   p.direct = rows_direct(dtype, d);
+  // Few queries: rows streamed past all of them, or tiles.  Streamed rows need no prepared copies and no LDS, and fp32
+  // ones are multiplied once instead of three times; tiles read a row's fragment once for 128 queries.  Streamed and tiles
+  // in us, k = 5: fp32 100,000 x 768, 16 queries 74 and 251, 64 queries 194 and 306; bf16 100,000 x 100 (copies) 64
+  // queries 34 and 60; bf16 100,000 x 768 (none) 16 queries 41 and 44, 32 queries 47 and 44, 64 queries 81 and 66;
+  // 100,000 x 320 32 queries 28 and 32, 64 queries 48 and 45.
+  p.few = nq <= (p.direct ? kSmFewQueries / 2 : kSmFewQueries);
   p.parts = (nb + kSmRecRows - 1) / kSmRecRows;
   p.keep_ld = round_up(nb, kSmTileRows);
-  // A record that holds two of the k best costs its 128 scores again, some 30 ns of the device a query, and k^2 / (2 parts)
-  // records do on average; a kept score costs 8 bytes of traffic, some 2 ps.  They break even near 8 records for each of
-  // the k.
-  p.keep = k > 0 && p.parts <= 8 * (int64_t)k;
+  // A record that holds two of the k best costs its 128 scores again, and k^2 / (2 parts) records do on average; kept scores
+  // cost 8 bytes of traffic each and a selection over all of them.  Recomputed and kept in us: 1000 queries, d = 128, bf16:
+  // 2500 rows, k = 10 (2 records for each of the k) 58 and 39, 4000 rows (3.1) 52 and 44, 10,000 rows, k = 20 (3.9) 65 and
+  // 63, k = 10 (7.8) 50 and 59, 65,536 rows, k = 64 (8) 182 and 952; 64 queries, 8000 rows, k = 32 (2) 88 and 38.
+  p.keep = k > 0 && p.parts <= 3 * (int64_t)k;
   const int64_t per = p.parts * (int64_t)sizeof(float4) + (p.keep ? p.keep_ld * 4 : 0);
   p.piece = std::min(nq, std::max<int64_t>(kSmTileQueries, per > 0 ? kPieceBytes / per / kSmTileQueries * kSmTileQueries : nq));
   p.kblocks = p.f.blocks(d);
@@ -95,7 +101,7 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
   const int64_t el = 2 * p.f.planes;
   const int64_t nqp = round_up(nq, kSmTileQueries), nbp = round_up(nb, kSmTileRows);
   p.chunk = std::min(nbp, std::max<int64_t>(kSmTileRows, kPieceBytes / (2 * el * nqp) / kSmTileRows * kSmTileRows));
-  p.small = sm_gradients_small(p.chunk, nq);
+  p.small = sm_gradients_small(p.f, p.chunk, nq, p.kblocks);
   p.tile_q = p.small ? 64 : kSmTileQueries;
   p.ld = round_up(d, 4);
   p.g_row = p.chunk * el;
@@ -128,7 +134,7 @@ GradPlan grad_plan(int64_t nb, int64_t nq, int d, int dtype) {
 }
 
 int check_rows(const char* who, int64_t nb, int64_t nq, int d, int dtype) {
-  if (d < 1) return fail(VS_ERR_INVALID_ARG, "%s: d = %d", who, d);
+  if (d < 1 || d > VS_MAX_ROW) return fail(VS_ERR_INVALID_ARG, "%s: d = %d outside [1, %d]", who, d, VS_MAX_ROW);
   if (nb < 0 || nb >= (int64_t)1 << 31) return fail(VS_ERR_INVALID_ARG, "%s: nb = %lld outside [0, 2^31)", who, (long long)nb);
   if (nq < 0 || nq >= (int64_t)1 << 31) return fail(VS_ERR_INVALID_ARG, "%s: nq = %lld outside [0, 2^31)", who, (long long)nq);
   if (dtype < VS_FP32 || dtype > VS_BF16) return fail(VS_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
@@ -163,6 +169,8 @@ int attend_space(const char* who, const vs_ivfpq* ix, int64_t nq, int dk, int v0
   if (v0 < 0 || v0 >= s.g.d || v0 % s.g.dsub) return fail(VS_ERR_INVALID_ARG, "%s: v0 = %d is not a multiple of %d in [0, %d)", who, v0, s.g.dsub, s.g.d);
   if (nprobe < 0 || nprobe > VS_MAX_K) return fail(VS_ERR_INVALID_ARG, "%s: nprobe = %d outside [0, %d]", who, nprobe, VS_MAX_K);
   o->nprobe = nprobe < s.g.nlist ? nprobe : 0;
+  int device = -1;
+  if (hipGetDevice(&device) != hipSuccess || device != s.device) return fail(VS_ERR_INVALID_ARG, "%s: the index is on device %d, the current device is %d", who, s.device, device);
   o->plan = attend_plan(s.g, s.ntotal, nq, dk, v0, dtype, o->nprobe, grad);
   if (!o->plan.fits) return fail(VS_ERR_UNSUPPORTED, "%s: the tables of M = %d, d = %d exceed the on-chip memory", who, s.g.M, s.g.d);
   if ((nq + o->plan.qb - 1) / o->plan.qb * o->plan.nsplit >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 workgroups", who);
@@ -183,6 +191,10 @@ int attend_run(const char* who, const vs_ivfpq* ix, AttendCall& c, const AttendS
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
   if (sp.nprobe > 0) {
+    // (a replay could meet the index's work space at another size, or in use by another call)
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone)
+      return fail(VS_ERR_UNSUPPORTED, "%s: probed lists under capture (the coarse quantizer uses the index's own work space)", who);
     float* q32 = reinterpret_cast<float*>(ws + sp.o_q32);
     int32_t* probes = reinterpret_cast<int32_t*>(ws + sp.o_probes);
     launch_attend_pad(c.q, c.nq, c.dk, c.ix->g.d, c.dtype, q32, st);

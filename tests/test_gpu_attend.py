@@ -110,6 +110,77 @@ def test_probed_lists(vs, dtype, d, M, dk, v0, coarse):
         check(mem, mem.queries(nq, dk, DTYPES[dtype]), nprobe, dk, v0)
 
 
+def codes_for_tiles(nq, mt, nlist_of=None, least=None):
+    """Stored vectors from which on nq queries go through the matrix cores (mt: look-ups a pair)."""
+    least = (16e6 if nq <= 16 else 48e6) if least is None else least
+    return int(least * (1 if nlist_of is None else 1 + 100.0 / (nlist_of - 8)) / (nq * mt)) + 77
+
+
+TILE_SHAPES = [s for s in SHAPES if s[0] != 768] + [(66, 22, 66, 0), (140, 28, 140, 5), (258, 86, 129, 129), (130, 26, 65, 65)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,M,dk,v0", TILE_SHAPES)
+def test_many_queries(vs, dtype, d, M, dk, v0):
+    """Enough work for the matrix cores: 16 queries a tile and 64, one list and lists of 90, some queries that see
+    nothing or little, a batch that ends inside a tile."""
+    mt = (dk + d - v0) * M // d
+    for nq, run in ((5, None), (16, 90), (17, None), (65, 90), (130, None)):
+        n = codes_for_tiles(nq, mt, run)
+        if n > 400_000 or n * d > 20_000_000:
+            continue
+        mem = Memory(vs, n, d, M, 1 if run is None else n // run, nq + d)
+        q = mem.queries(nq, dk, DTYPES[dtype])
+        check(mem, q, 0, dk, v0)
+        limits = torch.randint(0, n + 1, (nq,), generator=mem.g)
+        limits[0], limits[1], limits[2], limits[3] = 0, 1, -5, n // 2 // 64 * 64
+        check(mem, q, 0, dk, v0, limits=limits.cuda())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("d,M,dk,v0,nq,least", [(320, 80, 320, 0, 20, 48e6), (384, 64, 66, 0, 70, 256e6), (512, 128, 512, 0, 16, 48e6)])
+def test_long_results(vs, dtype, d, M, dk, v0, nq, least):
+    mem = Memory(vs, codes_for_tiles(nq, (dk + d - v0) * M // d, None, least), d, M, 1, d)
+    check(mem, mem.queries(nq, dk, DTYPES[dtype]), 0, dk, v0)
+
+
+@pytest.mark.parametrize("nq", [16, 100])
+def test_many_queries_on_lists_of_all_lengths(vs, nq):
+    """Lists that are empty, of one vector, of a tile and one more or less, among long ones; ids in another order."""
+    g = torch.Generator().manual_seed(15)
+    d, M, nlist = 32, 16, 200
+    sizes = [25000, 0, 1, 0, 0, 63, 64, 65, 128, 30000, 2049] + [int(v) for v in torch.randint(0, 130, (nlist - 11,), generator=g)]
+    own = torch.repeat_interleave(torch.arange(nlist), torch.tensor(sizes))
+    own = own[torch.randperm(own.numel(), generator=g)]
+    mem = Memory(vs, 0, d, M, nlist, 5, coarse=0)
+    ids = torch.randperm(own.numel(), generator=g)
+    mem.ix.add((mem.centroids[own] + torch.randn(own.numel(), d, generator=g) * 0.05).cuda(), ids.cuda())
+    got, lists = mem.ix.assignments()
+    mem.ids, mem.lists = got.cpu(), lists.long().cpu()
+    mem.rows = decode(f64(mem.centroids), f64(mem.codebooks), mem.ix.codes().cpu(), mem.lists)
+    q = mem.queries(nq, d, torch.float32)
+    check(mem, q, 0, d, 0)
+    check(mem, q, 0, d, 0, limits=torch.randint(0, own.numel(), (nq,), generator=g).cuda())
+    check(mem, q, 0, d, 0, limits=torch.full((nq,), 3).cuda())
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 40.0])
+def test_many_queries_flat_and_sharp(vs, scale):
+    mem = Memory(vs, 12_000, 64, 32, 3, 8)
+    check(mem, mem.queries(70, 64, torch.float32), 0, 64, 0, scale=scale)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** 20])
+def test_many_queries_magnitudes(vs, size):
+    mem = Memory(vs, 25_000, 32, 16, 2, 9, size=size)
+    q = (mem.queries(64, 32, torch.float32).clamp(-8, 8) / size).contiguous()
+    out, lse = mem.ix.attend(q, 0, 0.1)
+    ro, rl, p = attend(mem.rows, q, mem.sees(q, 0, None), 32, 0, 0.1)
+    es, tol = attend_tolerance(mem.rows / size, q * size, p, 32, 0, 0.1, mem.M, q.dtype, ro / size)
+    assert ((out.double().cpu() - ro).abs() / size <= tol).all()
+    assert ((lse.double().cpu() - rl).abs() <= es + 25_064 * 2.0 ** -24 + 2.0 ** -20 * float(rl.abs().amax())).all()
+
+
 @pytest.mark.parametrize("nprobe", [0, 5])
 @pytest.mark.parametrize("nq", [1, 2, 17, 130])
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -202,7 +273,7 @@ def test_gradient_agrees_with_differences(vs):
 
 def test_equal_calls_give_equal_bits_on_any_stream(vs):
     mem = Memory(vs, 9000, 128, 32, 50, 11)
-    for nq, nprobe, dtype in ((1, 0, "fp32"), (100, 0, "bf16"), (100, 8, "fp32")):
+    for nq, nprobe, dtype in ((1, 0, "fp32"), (100, 0, "bf16"), (200, 0, "fp32"), (100, 8, "fp32")):
         q = mem.queries(nq, 128, DTYPES[dtype])
         go = torch.randn(nq, 128, device="cuda").to(q.dtype)
         run = lambda: mem.ix.attend(q, nprobe, 0.1)
@@ -220,16 +291,16 @@ def test_equal_calls_give_equal_bits_on_any_stream(vs):
                 assert torch.equal(u, v)
 
 
-@pytest.mark.parametrize("nq,nprobe", [(1, 0), (40, 0), (6, 5)])
-def test_captured_and_replayed(vs, nq, nprobe):
-    mem = Memory(vs, 4000, 64, 32, 20, 12)
+@pytest.mark.parametrize("nq,n", [(1, 4000), (40, 4000), (40, 20_000)])
+def test_captured_and_replayed(vs, nq, n):
+    mem = Memory(vs, n, 64, 32, 20, 12)
     q = mem.queries(nq, 64, torch.bfloat16)
     go = torch.randn(nq, 64, device="cuda").bfloat16()
     limits = torch.full((nq,), 3000, device="cuda")
 
     def both():
-        o, z = mem.ix.attend(q, nprobe, 0.1, limits=limits)
-        return o, z, mem.ix.attend_grad(q, nprobe, 0.1, z, go, limits=limits)
+        o, z = mem.ix.attend(q, 0, 0.1, limits=limits)
+        return o, z, mem.ix.attend_grad(q, 0, 0.1, z, go, limits=limits)
 
     both()
     torch.cuda.synchronize()
@@ -246,6 +317,24 @@ def test_captured_and_replayed(vs, nq, nprobe):
         torch.cuda.synchronize()
         for u, v in zip(out, want):
             assert torch.equal(u, v)
+
+
+def test_probed_lists_are_refused_under_capture(vs):
+    """The coarse quantizer's work space is the index's own: a replay could meet it at another size or in use."""
+    mem = Memory(vs, 1000, 64, 32, 20, 12)
+    q = mem.queries(4, 64, torch.float32)
+    want = mem.ix.attend(q, 5, 0.1)
+    go = torch.ones_like(q)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        for call in (lambda: mem.ix.attend(q, 5, 0.1), lambda: mem.ix.attend_grad(q, 5, 0.1, want[1], go)):
+            with pytest.raises(vs.VSError) as e:
+                call()
+            assert e.value.code == -2
+        all_lists = mem.ix.attend(q, 20, 0.1)
+    assert all_lists[0].shape == q.shape
+    for u, v in zip(want, mem.ix.attend(q, 5, 0.1)):
+        assert torch.equal(u, v)
 
 
 def test_search_and_attention_share_an_index(vs):

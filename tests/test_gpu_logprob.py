@@ -59,7 +59,8 @@ def check_forward(vs, x, q, targets, k, scale, bias):
 # anywhere); kept scores (few records for the k) and records; records that hold several of the best
 SHAPES = [(1, 1, 1, 1), (2, 1, 7, 3), (129, 3, 33, 5), (500, 16, 128, 10), (1000, 17, 100, 1), (3000, 33, 65, 64),
           (20_000, 5, 768, 3), (40_000, 64, 48, 40), (127, 65, 64, 5), (128, 128, 256, 0), (129, 129, 31, 2),
-          (5000, 300, 96, 9), (60_001, 130, 64, 7), (300, 70, 1030, 4)]
+          (5000, 300, 96, 9), (60_001, 130, 64, 7), (300, 70, 1030, 4), (100_000, 5, 64, 20), (30_000, 33, 128, 17),
+          (2000, 32, 320, 5), (2100, 33, 320, 5), (2000, 64, 100, 40), (257, 256, 64, 64)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -162,6 +163,16 @@ def test_gradients(vs, dtype, nb, nq, d, masked):
     check_grad(vs, x, q, targets, lse, ent, 0.25, bias, 2)
 
 
+# what is tiled in larger tiles: pairs of long 16-bit rows; a gradient of many rows, stored as it is summed; one of few
+# tiles whose sums are long
+@pytest.mark.parametrize("dtype,nb,nq,d", [("bf16", 4100, 2100, 640), ("fp16", 4097, 2049, 700), ("bf16", 41_000, 130, 100),
+                                           ("fp32", 41_003, 70, 33), ("fp32", 8200, 4000, 600)])
+def test_large_gradients(vs, dtype, nb, nq, d):
+    x, q, targets, bias = make(nb, nq, d, DTYPES[dtype], 2, True, nb + d, grid=False)
+    ref = logprob(x, q, targets, 0, 0.1, bias)
+    check_grad(vs, x, q, targets, ref["lse"].float().cuda(), ref["entropy"].float().cuda(), 0.1, bias, 2)
+
+
 def test_gradients_in_chunks(vs):
     """More pairs than one piece of G holds: rows are taken in several chunks, queries' sums go on across them."""
     x, q, targets, bias = make(70_001, 1100, 24, torch.float32, 2, True, 9, grid=False)
@@ -207,6 +218,23 @@ def test_same_target_twice_and_padded_queries(vs):
     close(dx, rx, tx, "dx")
     close(db, rb, tb, "dbias")
     assert (dq[2] == 0).all() and (dq[5] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nb,d", [(300, 100), (4100, 640)])
+def test_padded_queries_among_many(vs, dtype, nb, d):
+    """A batch whose last third is padding: targets of -1, no gradients, whatever it holds."""
+    nq, live = 2100 if nb > 1000 else 90, 1400 if nb > 1000 else 60
+    x, q, targets, _ = make(nb, nq, d, DTYPES[dtype], 1, False, 21, grid=False)
+    q[live::2], q[live + 1::2] = float("nan"), INF
+    targets[live:] = -1
+    lse = vs.vs_flat_logprob(x, q, targets, scale=0.1)[1]
+    g = torch.ones(nq, 1, device="cuda")
+    dx, dq, db = vs.vs_flat_logprob_grad(x, q, lse, targets, g, scale=0.1)
+    ref = logprob_grad(x, q[:live], targets[:live], lse[:live], None, g[:live], None, None, 0.1, None)
+    for got, want, tol, what in zip((dq[:live], dx, db), *ref, ("dq", "dx", "dbias")):
+        close(got, want, tol, what)
+    assert (dq[live:] == 0).all()
 
 
 def test_only_what_is_wanted(vs):
