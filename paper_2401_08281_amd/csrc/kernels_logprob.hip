@@ -1,7 +1,7 @@
 // Softmax over the rows of a matrix: scores on the matrix cores with the softmax statistics in the
 // epilogue (the nq x nb scores are never stored), and the gradients, which compute them again.
 //
-// Orientation.  A tile is 128 rows of x (operand A) by 128 queries (operand B): in the accumulators of
+// Orientation.  Rows of x are operand A of a tile, queries operand B: in the accumulators of
 // v_mfma_f32_32x32x16 a lane then holds ONE query (column = lane & 31) and 16 rows per block
 // (row = (r & 3) + 8 (r >> 2) + 4 (lane >> 5)), so maxima and sums over rows are register arithmetic with a single
 // exchange between lane and lane ^ 32.
@@ -50,7 +50,7 @@ __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 // The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
 // not wait for them, and the compiler, which counts the wait states in between, has left them out where it copied an
 // accumulator at the start of the block behind the loop (v_accvgpr_read one instruction after the product: a stale
-// value).  20 wait states cover the 16 passes of a 32x32x16 product.
+// value).  A 32x32x16 product's 8 passes are over after 12 wait states, any other one's here after fewer than 20.
 __device__ __forceinline__ void settle_products() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
@@ -64,7 +64,8 @@ __device__ __forceinline__ void settle_products() {
 // and two workgroups a CU fill each other's waits and run one's epilogue beside the other's products.  A row's four 16-byte
 // pieces are stored at piece ^ ((row >> 2) & 3): a fragment read (32 rows x 2 pieces) then touches every bank evenly.
 // With two planes a unit holds 16 heads and their 16 tails, and one stage feeds hi*hi + hi*lo + lo*hi.
-// Against tiles of 128 x 128 by 64 x 64 (K units of 128 bytes), scores of 4096 x 65,536 x 768: measured beside the kernel.
+// Against tiles of 128 x 128 by 64 x 64 (K units of 128 bytes): bf16 4096 x 65,536 x 768 with its finish 579 us for 616,
+// fp32 1000 x 200,003 x 100 348 for 417.
 // Products and gradients of few tiles take 128 x 64 by 64 x 32 instead (IB, JB: 32-row and 32-query blocks of a wavefront).
 constexpr int kTileA = 256, kTileB = 128;
 template <int IB, int JB>
@@ -229,7 +230,9 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
 
 // ---- forward: scores -> softmax records ---------------------------------------------
 // Bound by the matrix cores for long vectors and by the epilogue's exponentials (some 12 vector instructions per score)
-// for short ones.  A wavefront's 128 rows are a record of each of its 64 queries.
+// for short ones: bf16 4096 x 65,536 x 768 445 to 520 us with the clock, 790 to 930 TFLOP/s (the library's product of these
+// sizes, stored, runs at 976); fp32 1000 x 200,003 x 100 in three products 246 us.  A wavefront's 128 rows are a record of
+// each of its 64 queries.
 template <int PLANES, bool BF16, bool SECOND>
 __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords R, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords
 // Up to 64 queries the rows are what there is to read: a wavefront loads fragments of 32 rows straight from memory
 // (no LDS, 16 bytes a lane and load) and multiplies them with all queries, whose fragments wait in LDS; four wavefronts
 // make the record of 128 rows.  fp32 rows use v_mfma_f32_16x16x4_f32: exact products, and its 157 TFLOP/s are far above
-// what the stream of rows can ask for.
+// what the stream of rows can ask for.  Bound by memory: bf16 100,003 x 768, one query, 32.8 us, 4.7 TB/s as a copy has.
 // In the 16x16 layouts a lane holds row lane & 15 of A, and of the result column lane & 15 and rows 4 (lane >> 4) + r.
 template <int DT>
 struct FewMul {
@@ -543,7 +546,8 @@ __device__ __forceinline__ void wave_take_best(const float4 (&rec)[kTakePer], in
 // can count unless its second best reaches the k-th best maximum: then its 128 scores are computed again in fp32.
 // Where that would be common (few records, or many alternatives) the scores have been kept, and are read instead.
 // TAKE: up to kTakeBest alternatives of up to 256 kTakePer records (262,144 rows), which stay in registers and are picked
-// one by one; more go through the reservoir selection, whose first sort alone takes some 700 instructions.
+// one by one; more go through the reservoir selection, whose first sort alone takes some 700 instructions.  A chain of
+// latencies: one query of 782 records, k = 10, 11.7 us; 4096 queries of 512 records, k = 5, 61 us.
 template <int DT, bool TAKE>
 __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R) {
   typedef typename Elem<DT>::T T;
@@ -720,7 +724,8 @@ __device__ __forceinline__ void load_piece(const T* __restrict__ row, int k, int
   }
 }
 
-// 16 lanes a row, 16 bytes a lane and step; rows of up to kPrepSteps steps are read once and stay in registers.
+// 16 lanes a row, 16 bytes a lane and step; rows of up to kPrepSteps steps are read once and stay in registers.  Bound by
+// memory: 201,003 x 100 fp32 into two planes 30 us, 183 MB at 6.1 TB/s (part of it stays in the last-level cache).
 constexpr int kPrepSteps = 8;
 template <int DT, int PLANES>
 __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d, int64_t dp) {
@@ -792,7 +797,7 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide 
 }
 
 // Largest size in every column: a thread goes down 16 bytes of columns.  (A maximum does not depend on the order, and
-// non-negative floats are ordered as their bits.)
+// non-negative floats are ordered as their bits.)  69,632 x 768 bf16: 67 us, 1.6 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void sm_colmax_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d, int64_t rows_per) {
   typedef typename Elem<DT>::T T;
@@ -827,7 +832,8 @@ __global__ __launch_bounds__(256) void sm_colmax_kernel(SmSide side0, SmSide sid
   }
 }
 
-// 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r, read and written in 16-byte pieces
+// 64 rows x 64 columns through LDS: column t becomes a row of K blocks over r, read and written in 16-byte pieces.
+// 69,632 x 768 bf16: 65 us, 214 MB at 3.3 TB/s.
 template <int DT, int PLANES>
 __global__ __launch_bounds__(256) void sm_prep_cols_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d) {
   typedef typename Elem<DT>::T T;
@@ -905,6 +911,7 @@ __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, in
 
 // Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
 // G / bound 2^14 in fp16: a value keeps 11 bits (22 with a tail) down to 2^-28 of the bound and 2^-38 of it below.
+// Bound by the matrix cores and the stores of G: bf16 4096 x 16,384 x 768 207 us, 500 TFLOP/s beside 268 MB at 1.3 TB/s.
 template <int PLANES, bool BF16, int IB, int JB>
 __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut O, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
@@ -1066,6 +1073,7 @@ __device__ __forceinline__ void store_4(void* p, int64_t i, int n, bool whole, i
 // out[b][a] = sum_k A[a][k] B[b][k] over long K: tiles of 256 x 256, eight wavefronts of 128 x 64 each.  Against 128 x 128
 // tiles a K block reads three quarters of the LDS per product, and its 2048 cycles of products a SIMD cover the way of the
 // next block from the last-level cache.  Fragments of the next 16 K elements are read while the present ones multiply.
+// 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 141 us: 710 and 730 TFLOP/s.
 constexpr int kBigTile = 256;
 constexpr int kBigStage = 2 * kBigTile * 128;
 // With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type.
