@@ -1335,6 +1335,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
   const int lane = lane_id(), wave = wave_id(), t = blockIdx.y * 64 + lane;
   const float* p = part + qi * nsplit * ld;
   float inv = 1.f;
+  bool nothing = false;                           // (backward) no row's weight: zeros, whatever the query and its gradients hold
   if (!GRAD) {
     float m = neg_inf();
     for (int s = threadIdx.x; s < nsplit; s += 256) m = fmaxf(m, p[s * ld]);
@@ -1369,7 +1370,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
     __syncthreads();
     mean = red[0] + red[1] + red[2] + red[3];
     total = red[4] + red[5] + red[6] + red[7];
-    if (total != 0.f) mean /= total;
+    nothing = total == 0.f;
+    if (!nothing) mean /= total;
     const float gl = g_lse ? g_lse[qi] : 0.f;
     for (int s = threadIdx.x; s < nsplit; s += 256) factor[s] = p[s * ld + 2] - mean + gl;
     inv = scale;
@@ -1399,7 +1401,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
   }
   sums[wave][lane] = v;
   __syncthreads();
-  if (wave == 0 && t < nout) store_as(out, qi * nout + t, dtype, (sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]) * inv);
+  if (wave == 0 && t < nout)
+    store_as(out, qi * nout + t, dtype, nothing ? 0.f : (sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]) * inv);
 }
 
 // q [nq, dk] of any type -> fp32 [nq, d] with zeros behind

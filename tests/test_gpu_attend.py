@@ -337,6 +337,36 @@ def test_probed_lists_are_refused_under_capture(vs):
         assert torch.equal(u, v)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nq,n,nprobe", [(2, 500, 0), (10, 4000, 3), (16, 30_000, 0), (70, 20_000, 0)])
+def test_padded_queries(vs, dtype, nq, n, nprobe):
+    """Queries of a batch that are padding, with a limit of 0 and anything inside, answer with zeros, and the others as
+    they do without them; a NaN query that sees rows does not reach the others either."""
+    mem = Memory(vs, n, 64, 32, 6, 17)
+    q = mem.queries(nq, 64, DTYPES[dtype])
+    limits = torch.full((nq,), n)
+    pad = torch.arange(1, nq, 3)
+    limits[pad] = 0
+    go = torch.randn(nq, 64, generator=mem.g).to(q.dtype).cuda()
+    gl = torch.randn(nq, generator=mem.g).cuda()
+    q[pad], go[pad] = 0, 0
+    out, lse = mem.ix.attend(q, nprobe, 0.1, limits=limits.cuda())
+    dq = mem.ix.attend_grad(q, nprobe, 0.1, lse, go, gl, limits=limits.cuda())
+    for bad in (float("nan"), INF, -INF, float(torch.finfo(q.dtype).max)):
+        q[pad], go[pad], gl[pad] = bad, bad, bad
+        o2, z2 = mem.ix.attend(q, nprobe, 0.1, limits=limits.cuda())
+        d2 = mem.ix.attend_grad(q, nprobe, 0.1, z2, go, gl, limits=limits.cuda())
+        assert (z2[pad] == -INF).all() and (o2[pad] == 0).all() and (d2[pad] == 0).all()
+        assert torch.equal(o2, out) and torch.equal(z2, lse) and torch.equal(d2, dq)
+    q[pad] = float("nan")
+    o2, z2 = mem.ix.attend(q, nprobe, 0.1)
+    live = torch.ones(nq, dtype=torch.bool)
+    live[pad] = False
+    assert torch.equal(o2[live], out[live]) and torch.equal(z2[live], lse[live])
+    if nprobe == 0:
+        assert z2[pad].isnan().all() and o2[pad].isnan().all()
+
+
 def test_search_and_attention_share_an_index(vs):
     """Attention leaves the index as it is, and a growing index is attended as it stands."""
     mem = Memory(vs, 2000, 64, 32, 16, 13)
