@@ -74,6 +74,9 @@ constexpr int tile_lds() { return 2 * 64 * (IB + JB) * 64; }
 template <int PLANES, bool BF16, int IB = 4, int JB = 2>
 struct TileMul {
   static constexpr int TA = 64 * IB, TB = 64 * JB, kStage = (TA + TB) * 64;
+  // The products with tails are summed apart where registers allow: added to the large sums one by one, each would leave a
+  // rounding of theirs (the gradient of a sharp softmax is what such roundings leave of 1 - p).
+  static constexpr bool kApart = PLANES == 2 && IB * JB <= 2;
   static __device__ __forceinline__ f32x16 mul(u32x4 a, u32x4 b, f32x16 c) {
     if constexpr (BF16)
       return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -121,6 +124,7 @@ struct TileMul {
     const int ra = (wa * 32 * IB + (lane & 31)) * 64, rb = TA * 64 + (wb * 32 * JB + (lane & 31)) * 64, half = lane >> 5, sw = (lane >> 2) & 3;
     request(0);
     const int n = (int)(ku1 - ku0);
+    f32x16 low[kApart ? IB : 1][kApart ? JB : 1] = {};
     for (int t = 0; t < n; ++t) {
       __syncthreads();                                  // the stage has landed, the other one is free
       const char* s = lds + (t & 1) * kStage;
@@ -143,12 +147,27 @@ struct TileMul {
       products(a[0], b[0]);
       if constexpr (PLANES == 1) {
         products(a[1], b[1]);
+      } else if constexpr (kApart) {
+#pragma unroll
+        for (int ib = 0; ib < IB; ++ib)
+#pragma unroll
+          for (int jb = 0; jb < JB; ++jb) {
+            low[ib][jb] = mul(a[0][ib], b[1][jb], low[ib][jb]);
+            low[ib][jb] = mul(a[1][ib], b[0][jb], low[ib][jb]);
+          }
+        settle_products();
       } else {
         products(a[0], b[1]);
         products(a[1], b[0]);
       }
     }
     __syncthreads();                                    // LDS is free for the epilogue
+    if constexpr (kApart) {
+#pragma unroll
+      for (int ib = 0; ib < IB; ++ib)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) acc[ib][jb] += low[ib][jb];
+    }
   }
 };
 
