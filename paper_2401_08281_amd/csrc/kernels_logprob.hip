@@ -487,11 +487,6 @@ __device__ __forceinline__ float wave_sum(float v) {
   for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
   return v;
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int w = 32; w > 0; w >>= 1) v = fmaxf(v, __shfl_xor(v, w));
-  return v;
-}
 
 // <q, x_j> for eight rows at once, eight lanes a row; every lane of a row's group gets the sum.  LANES = 64: one row.
 template <int LANES, typename T>
