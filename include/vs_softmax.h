@@ -64,7 +64,8 @@ VS_API int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq,
  *   out_dq [nq, d], out_dx [nb, d] of `dtype`, out_dbias [nb] fp32: each may be NULL (not wanted).
  * G is held in fp16 relative to a bound of its row (for fp32 vectors in two parts, together 22 bits), 2^-11 of a value
  * or 2^-38 of the bound; sums are fp32.
- * Errors: as vs_flat_logprob; entropy missing where g_entropy is given.  nq = 0 sets out_dx and out_dbias to zero.
+ * Errors: as vs_flat_logprob; entropy missing where g_entropy is given; VS_ERR_UNSUPPORTED beyond 2^23 tiles of 128 rows or
+ * components by 64 queries.  nq = 0 sets out_dx and out_dbias to zero.
  */
 VS_API int64_t vs_flat_logprob_grad_workspace_bytes(int64_t nb, int64_t nq, int32_t d, int32_t dtype);
 VS_API int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, int32_t d, int32_t dtype, float scale,

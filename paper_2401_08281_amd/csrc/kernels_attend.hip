@@ -218,8 +218,10 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
   const int d = A.g.d, dsub = A.g.dsub, M = A.g.M, cs = A.g.code_size, dv = d - A.v0;
   const int mk = A.dk / dsub, mv = dv / dsub, mv0 = M - mv;
   const int h0 = GRAD ? 0 : mv0, hd0 = GRAD ? 0 : A.v0, nout = GRAD ? A.dk : dv;   // the histogrammed sub-quantizers
-  const int split = blockIdx.x % A.nsplit;
-  const int64_t q0 = (int64_t)(blockIdx.x / A.nsplit) * QB;
+  const u32 wg = (u32)group_id();                              // (below 2^31)
+  const int split = wg % A.nsplit;
+  const int64_t q0 = (int64_t)(wg / A.nsplit) * QB;
+  if (q0 >= A.nq) return;
   Segment* segs = reinterpret_cast<Segment*>(lds + L.seg);
   int* ctl = reinterpret_cast<int*>(lds + L.seg + (int)(sizeof(Segment) / 4) * kSegments);   // {segments, rows, next candidate, -, offset (two words), runs}
   int64_t* offset = reinterpret_cast<int64_t*>(ctl + 4);         // rows of the next candidate that are done
@@ -909,8 +911,10 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   const int mk = A.dk / dsub, mv = dv / dsub, mv0 = M - mv;
   const CodeSet K = code_set(0, mk, dsub, W), V = code_set(mv0, mv, dsub, W);
   const int nout = GRAD ? A.dk : dv, om0 = GRAD ? 0 : mv0, mo = GRAD ? mk : mv;
-  const int split = blockIdx.x % A.nsplit;
-  const int64_t q0 = (int64_t)(blockIdx.x / A.nsplit) * QT;
+  const u32 wg = (u32)group_id();                              // (below 2^31)
+  const int split = wg % A.nsplit;
+  const int64_t q0 = (int64_t)(wg / A.nsplit) * QT;
+  if (q0 >= A.nq) return;
   const int64_t r0 = split * A.per, r1 = r0 + A.per < A.ntotal ? r0 + A.per : A.ntotal;
   float* red = reinterpret_cast<float*>(ldsb + L.red);
   float* stat = reinterpret_cast<float*>(ldsb + L.stat);     // per query: up, down of q; up, down of g; bound of w; bias
@@ -1325,13 +1329,14 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
 // parts' factors come first, a part a thread; then four wavefronts go through the parts, eight loads in flight each.
 constexpr int kMaxParts = 2048;
 template <bool GRAD>
-__global__ __launch_bounds__(256) void attend_join_kernel(const float* __restrict__ part, int nsplit, int64_t ld, int nout,
+__global__ __launch_bounds__(256) void attend_join_kernel(const float* __restrict__ part, int64_t nq, int nsplit, int64_t ld, int nout,
                                                           const float* __restrict__ g_lse, float scale, int dtype,
                                                           void* __restrict__ out, float* __restrict__ out_lse) {
   __shared__ float factor[kMaxParts];
   __shared__ float red[8];
   __shared__ float sums[4][64];
-  const int64_t qi = blockIdx.x;
+  const int64_t qi = blockIdx.x + (int64_t)gridDim.x * blockIdx.z;
+  if (qi >= nq) return;
   const int lane = lane_id(), wave = wave_id(), t = blockIdx.y * 64 + lane;
   const float* p = part + qi * nsplit * ld;
   float inv = 1.f;
@@ -1408,7 +1413,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const float* __restric
 // q [nq, dk] of any type -> fp32 [nq, d] with zeros behind
 __global__ __launch_bounds__(256) void attend_pad_kernel(const void* __restrict__ q, int64_t nq, int dk, int d, int dtype,
                                                          float* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = group_id() * 256 + threadIdx.x;
   if (i >= nq * d) return;
   const int64_t r = i / d;
   const int t = (int)(i - r * d);
@@ -1488,14 +1493,14 @@ AttendPlan attend_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, i
 }
 
 void launch_attend_pad(const void* q, int64_t nq, int dk, int d, int dtype, float* out, hipStream_t st) {
-  attend_pad_kernel<<<(unsigned)((nq * d + 255) / 256), 256, 0, st>>>(q, nq, dk, d, dtype, out);
+  attend_pad_kernel<<<grid_2d((nq * d + 255) / 256), 256, 0, st>>>(q, nq, dk, d, dtype, out);
 }
 
 void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* part, hipStream_t st) {
   const IvfStore& s = *c.ix;
   ScanArgs a{s.g, s.centroids, s.codebooks, s.codes, s.ids, s.list_off, s.ntotal, c.q, c.nq, c.dk, c.v0, c.dtype, c.scale,
              c.limits, c.probes, c.nprobe, p.nsplit, p.per, c.lse, c.g_out, part, p.ld};
-  const unsigned g = (unsigned)((c.nq + p.qb - 1) / p.qb * p.nsplit);
+  const dim3 g = grid_2d((c.nq + p.qb - 1) / p.qb * p.nsplit);
   auto run = [&](auto kern) {
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
     kern<<<g, 256, p.lds, st>>>(a);
@@ -1533,7 +1538,7 @@ void launch_attend(const AttendCall& c, const AttendPlan& p, bool grad, float* p
     }
 #undef SCAN
   }
-  const dim3 gj((unsigned)c.nq, (unsigned)((p.nout + 63) / 64));
-  if (grad) attend_join_kernel<true><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, c.g_lse, c.scale, c.dtype, c.out, nullptr);
-  else attend_join_kernel<false><<<gj, 256, 0, st>>>(part, p.nsplit, p.ld, p.nout, nullptr, c.scale, c.dtype, c.out, c.out_lse);
+  const dim3 gq = grid_2d(c.nq), gj(gq.x, (unsigned)((p.nout + 63) / 64), gq.y);
+  if (grad) attend_join_kernel<true><<<gj, 256, 0, st>>>(part, c.nq, p.nsplit, p.ld, p.nout, c.g_lse, c.scale, c.dtype, c.out, nullptr);
+  else attend_join_kernel<false><<<gj, 256, 0, st>>>(part, c.nq, p.nsplit, p.ld, p.nout, nullptr, c.scale, c.dtype, c.out, c.out_lse);
 }

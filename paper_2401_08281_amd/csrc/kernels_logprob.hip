@@ -361,7 +361,8 @@ __global__ __launch_bounds__(256) void sm_scores_few_kernel(const typename Elem<
   extern __shared__ __align__(16) char lds[];
   u32x4* frag = reinterpret_cast<u32x4*>(lds);        // [step][NT][64]
   const int lane = lane_id(), wave = wave_id(), g = lane >> 4;
-  const int64_t part = blockIdx.x, j0 = part * kSmRecRows + wave * 32;
+  const int64_t part = group_id(), j0 = part * kSmRecRows + wave * 32;
+  if (part >= R.parts) return;
   const typename F::T* row[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -570,7 +571,8 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
   __shared__ u64 chosen[VS_MAX_TOP];
   __shared__ u64 shared_bound;
   __shared__ float red[3][4];
-  const int64_t qi = blockIdx.x;
+  const int64_t qi = group_id();
+  if (qi >= F.nq) return;
   const int lane = lane_id(), wave = wave_id();
   const float4* rec = R.rec + qi * R.parts;
   const T* x = static_cast<const T*>(F.x);
@@ -745,12 +747,13 @@ template <int DT, int PLANES>
 __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide side1, unsigned blocks0, int d, int64_t dp) {
   typedef typename Elem<DT>::T T;
   constexpr int V = 16 / sizeof(T);
-  const SmSide& S = blockIdx.x < blocks0 ? side0 : side1;
+  const int64_t wg = group_id();
+  const SmSide& S = wg < blocks0 ? side0 : side1;
   const T* __restrict__ x = static_cast<const T*>(S.x);
   const float* __restrict__ bias = S.bias;
   char* __restrict__ planes = static_cast<char*>(S.rows);
   float* __restrict__ scale = S.row_scale;
-  const int64_t r = (int64_t)(blockIdx.x < blocks0 ? blockIdx.x : blockIdx.x - blocks0) * 16 + (threadIdx.x >> 4);
+  const int64_t r = (wg < blocks0 ? wg : wg - blocks0) * 16 + (threadIdx.x >> 4);
   if (r >= S.n) return;                                                // (whole groups of 16 lanes)
   const int l = threadIdx.x & 15;
   const bool gone = bias && bias[r] == neg_inf(), kept = dp <= 16 * V * kPrepSteps;
@@ -889,7 +892,8 @@ __global__ __launch_bounds__(256) void sm_prep_cols_kernel(SmSide side0, SmSide 
   typedef typename Elem<DT>::T T;
   constexpr int V = 16 / sizeof(T);
   __shared__ float tile[64][65];
-  const SmSide& S = blockIdx.x < blocks0 ? side0 : side1;
+  const int64_t wg = blockIdx.x + (int64_t)gridDim.x * blockIdx.z;
+  const SmSide& S = wg < blocks0 ? side0 : side1;
   const T* __restrict__ x = static_cast<const T*>(S.x);
   const float* __restrict__ bias = S.bias;
   const float* __restrict__ factor = S.factor;
@@ -897,7 +901,7 @@ __global__ __launch_bounds__(256) void sm_prep_cols_kernel(SmSide side0, SmSide 
   char* __restrict__ planes = static_cast<char*>(S.cols);
   float* __restrict__ scale = S.col_scale;
   const int64_t n = S.n, np = S.np;
-  const int64_t r0 = (int64_t)(blockIdx.x < blocks0 ? blockIdx.x : blockIdx.x - blocks0) * 64;
+  const int64_t r0 = (wg < blocks0 ? wg : wg - blocks0) * 64;
   const int t0 = blockIdx.y * 64;
   for (int i = threadIdx.x; i < 64 * 64 / V; i += 256) {
     const int row = i / (64 / V), c = i % (64 / V) * V;
@@ -1276,7 +1280,7 @@ __global__ __launch_bounds__(256) void sm_product_out_kernel(const float* __rest
                                                              int64_t ld, int d, const float* __restrict__ sa,
                                                              const float* __restrict__ sb, float alpha,
                                                              typename Elem<DT>::T* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = group_id() * 256 + threadIdx.x;
   if (i >= rows * d) return;
   const int64_t b = i / d;
   const int a = (int)(i - b * d);
@@ -1320,8 +1324,9 @@ void launch_sm_zero(void* p, int64_t bytes, hipStream_t st) {
 
 void launch_sm_prep_rows(const SmForm& f, const SmSide& a, const SmSide& b, int d, hipStream_t st) {
   const int64_t dp = f.blocks(d) * f.per_block();
-  const unsigned ga = grid_of(a.n, 16), g = ga + grid_of(b.n, 16);
-  if (g == 0) return;
+  const unsigned ga = grid_of(a.n, 16), n = ga + grid_of(b.n, 16);
+  if (n == 0) return;
+  const dim3 g = grid_2d(n);
   if (f.dtype == 0) sm_prep_rows_kernel<0, 2><<<g, 256, 0, st>>>(a, b, ga, d, dp);
   else if (f.dtype == 1) sm_prep_rows_kernel<1, 1><<<g, 256, 0, st>>>(a, b, ga, d, dp);
   else sm_prep_rows_kernel<2, 1><<<g, 256, 0, st>>>(a, b, ga, d, dp);
@@ -1338,7 +1343,8 @@ void prep_cols(SmSide a, SmSide b, const SmForm& f, int d, hipStream_t st) {
   const unsigned ya = grid_of(a.n, (int)per), y = ya + grid_of(b.n, (int)per);
   sm_colmax_kernel<DT><<<dim3(grid_of(d, 64 * 16 / (int)sizeof(T)), y), 256, 0, st>>>(a, b, ya, d, per);
   const unsigned xa = grid_of(a.np, 64), x = xa + grid_of(b.np, 64);
-  sm_prep_cols_kernel<DT, PLANES><<<dim3(x, grid_of(d, 64)), 256, 0, st>>>(a, b, xa, d);
+  const dim3 g = grid_2d(x);
+  sm_prep_cols_kernel<DT, PLANES><<<dim3(g.x, grid_of(d, 64), g.y), 256, 0, st>>>(a, b, xa, d);
 }
 }  // namespace
 
@@ -1363,7 +1369,7 @@ template <int DT, int NT>
 void scores_few(const void* x, int64_t nb, const void* q, int64_t nq, int d, float scale, const float* bias,
                 const SmRecords& r, bool second, hipStream_t st) {
   typedef typename Elem<DT>::T T;
-  const unsigned g = grid_of(nb, kSmRecRows);
+  const dim3 g = grid_2d(r.parts);
   const int chunk = few_chunk<DT, NT>(), steps = ((d < chunk ? d : chunk) + FewMul<DT>::KS - 1) / FewMul<DT>::KS;
   const int recs = 4 * NT * 16 * 20, frags = steps * NT * 1024, lds = frags > recs ? frags : recs;
   if (second)
@@ -1389,7 +1395,7 @@ void launch_sm_scores_few(int dtype, const void* x, int64_t nb, const void* q, i
 }
 
 void launch_sm_finish(const SmFinish& f, const SmRecords& r, hipStream_t st) {
-  const unsigned g = (unsigned)f.nq;
+  const dim3 g = grid_2d(f.nq);
   const bool take = f.k <= kTakeBest && r.parts <= 256 * kTakePer && !r.keep;
   auto run = [&](auto some, auto all) {
     if (take) some<<<g, 256, 0, st>>>(f, r);
@@ -1446,6 +1452,7 @@ SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks) {
   if (want > most) want = most;
   if (want > 16) want = 16;
   p.splits = want < 1 ? 1 : (int)want;
+  p.groups = n * p.splits;
   return p;
 }
 
@@ -1482,7 +1489,7 @@ void launch_sm_product_direct(const SmForm& f, const SmMatrix& A, const SmMatrix
 
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* sa, const float* sb,
                            float alpha, int dtype, void* out, hipStream_t st) {
-  const unsigned g = grid_of(rows * d, 256);
+  const dim3 g = grid_2d((rows * d + 255) / 256);
   if (dtype == 0) sm_product_out_kernel<0><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<float*>(out));
   else if (dtype == 1) sm_product_out_kernel<1><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<_Float16*>(out));
   else sm_product_out_kernel<2><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<__bf16*>(out));

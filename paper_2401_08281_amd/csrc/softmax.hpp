@@ -6,6 +6,14 @@
 #include "internal.hpp"
 #include "store.hpp"
 
+// A launch of n workgroups: in two dimensions from 2^23 on, since HIP drops, without an error, what goes beyond 2^32
+// threads of one dimension.  The workgroups past the n-th have nothing to do.
+constexpr int64_t kGroupsInRow = (int64_t)1 << 23;
+inline dim3 grid_2d(int64_t n) {
+  return n <= kGroupsInRow ? dim3((unsigned)n) : dim3((unsigned)kGroupsInRow, (unsigned)((n + kGroupsInRow - 1) / kGroupsInRow));
+}
+__device__ __forceinline__ int64_t group_id() { return blockIdx.x + (int64_t)gridDim.x * blockIdx.y; }
+
 // ---- log-probabilities over rows (kernels_logprob.hip) ---------------------------
 // A matrix as the matrix cores read it: rows of whole 128-byte K blocks (two units of 64 bytes), `rows` of them that
 // exist.  A K unit holds 32 fp16 or bf16 elements, or (planes == 2) 16 fp16 heads and behind them their 16 fp16 tails.
@@ -83,7 +91,10 @@ struct SmGOut {
 bool sm_gradients_small(const SmForm& f, int64_t nx, int64_t nq, int64_t kblocks);
 void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const SmGOut& o, hipStream_t st);
 // out[b][a] (+)= sum_k A[a][k] B[b][k], K blocks split over workgroups: part[split][b][ld]
-struct SmProductPlan { bool big; int splits; };
+struct SmProductPlan {
+  bool big; int splits;
+  int64_t groups;                   // workgroups, of pieces of fewer rows fewer
+};
 SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks);
 void launch_sm_product(const SmForm& f, const SmProductPlan& p, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, bool add,
                        float* part, int64_t ld, hipStream_t st);

@@ -235,8 +235,6 @@ int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq, int32_
   if (misaligned(x, 16) || misaligned(q, 16)) return fail(VS_ERR_INVALID_ARG, "%s: x and q have to be 16-byte aligned", who);
   const LogprobPlan p = logprob_plan(nb, nq, d, dtype, k);
   if (int rc = check_space(who, workspace, workspace_bytes, p.bytes)) return rc;
-  if (p.parts * ((p.piece + kSmTileQueries - 1) / kSmTileQueries) >= (int64_t)1 << 31)
-    return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
   SmScores s;
@@ -304,7 +302,10 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     return fail(VS_ERR_INVALID_ARG, "%s: x and q have to be 16-byte aligned, their gradients 4-byte", who);
   const GradPlan p = grad_plan(nb, nq, d, dtype);
   if (int rc = check_space(who, workspace, workspace_bytes, p.bytes)) return rc;
-  if ((nq + 63) / 64 * (p.chunk / kSmTileRows) >= (int64_t)1 << 31) return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^31 tiles", who);
+  // (far beyond what the work space of such a call leaves of the memory)
+  const int64_t tiles = round_up(nq, p.tile_q) / p.tile_q * (p.chunk / (p.small ? 128 : kSmTileRows));
+  if (std::max(tiles, std::max(p.to_q.groups, p.to_x.groups)) >= kGroupsInRow)
+    return fail(VS_ERR_UNSUPPORTED, "%s: more than 2^23 tiles", who);
   if (!out_dq && !out_dx && !out_dbias) return VS_OK;
   char* ws = static_cast<char*>(workspace);
   auto at = [&](int64_t o) { return reinterpret_cast<float*>(ws + o); };
