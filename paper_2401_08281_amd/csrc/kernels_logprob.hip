@@ -523,6 +523,10 @@ __device__ __forceinline__ float wave_max_dpp(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// A score as what it is ordered by: keys tell zeros of different signs apart, which are equal scores (a negative scale, a
+// scale of zero and a bias of -0 make such).
+__device__ __forceinline__ float rank_value(float s) { return s + 0.f; }
+
 constexpr int kTakeBest = 16, kTakePer = 8;
 // The k best of the wavefront's records (thread's i-th: threadIdx.x + 256 i) as ascending keys of {maximum, record}: the
 // best of the lanes' bests k times, its lane going through its own again.
@@ -586,6 +590,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
     for (int i = 0; i < kTakePer; ++i) {
       const int64_t p = threadIdx.x + 256 * i;
       own[i] = p < R.parts ? rec[p] : make_float4(neg_inf(), 0.f, 0.f, 0.f);
+      own[i].x = rank_value(own[i].x);
     }
 #pragma unroll
     for (int i = 0; i < kTakePer; ++i) m = fmaxf(m, own[i].x);
@@ -647,7 +652,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
     const float* s = R.keep + qi * R.keep_ld;
     for (int64_t j0 = wave * 64; j0 < F.nb; j0 += 256) {
       const int64_t j = j0 + lane;
-      const float v = j < F.nb ? s[j] : neg_inf();
+      const float v = j < F.nb ? rank_value(s[j]) : neg_inf();
       sel.push_value(v > neg_inf(), v, (u32)j);
     }
   } else {
@@ -655,7 +660,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
       start();
       for (int64_t p0 = wave * 64; p0 < R.parts; p0 += 256) {
         const int64_t p = p0 + lane;
-        const float v = p < R.parts ? rec[p].x : neg_inf();
+        const float v = p < R.parts ? rank_value(rec[p].x) : neg_inf();
         sel.push_value(v > neg_inf(), v, (u32)p);
       }
       sel.finish();
@@ -697,7 +702,7 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
           const int64_t j = (int64_t)pw * kSmRecRows + r0 + group;
           const bool in = j < F.nb;
           const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
-          const float s = dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b;
+          const float s = rank_value(dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b);
           sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
         }
       }
