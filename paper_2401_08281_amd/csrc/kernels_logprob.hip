@@ -687,24 +687,27 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
     const u32 p = key_index(key);
     const float w = key != KEY_EMPTY ? rec[p].w : 0.f;
     const bool whole = key != KEY_EMPTY && w >= tau;
-    const u64 alone = make_key(key_value(key, 1), p * kSmRecRows + (__float_as_uint(w) & 127u), 1);
+    const u32 lone_row = p * kSmRecRows + (__float_as_uint(w) & 127u);
     const u64 todo = __ballot(whole);
     __syncthreads();                                        // (everybody has read what was chosen)
     if (todo == 0) {                                        // the maxima are the best rows, in this order
-      if (wave == 0 && lane < F.k) chosen[lane] = key == KEY_EMPTY ? KEY_EMPTY : alone;
+      if (wave == 0 && lane < F.k) chosen[lane] = key == KEY_EMPTY ? KEY_EMPTY : make_key(key_value(key, 1), lone_row, 1);
       done = true;
     } else {
+      // (the maxima that stand alone are multiplied again as well: equal rows must meet with equal bits)
       start();
-      if (wave == 0) sel.push(key != KEY_EMPTY && !whole, alone);
+      auto again = [&](int64_t j, bool in) {
+        in = in && j < F.nb;
+        const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
+        const float s = rank_value(dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b);
+        sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
+      };
+      const u64 lone = __ballot(key != KEY_EMPTY && !whole);
+      for (int i0 = wave * 8; i0 < F.k; i0 += 32)
+        again(__shfl(lone_row, i0 + group), (lone >> (i0 + group)) & 1u);
       for (u64 rest = todo; rest; rest &= rest - 1) {
         const u32 pw = __shfl(p, __ffsll(rest) - 1);
-        for (int r0 = wave * 8; r0 < kSmRecRows; r0 += 32) {
-          const int64_t j = (int64_t)pw * kSmRecRows + r0 + group;
-          const bool in = j < F.nb;
-          const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
-          const float s = rank_value(dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b);
-          sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
-        }
+        for (int r0 = wave * 8; r0 < kSmRecRows; r0 += 32) again((int64_t)pw * kSmRecRows + r0 + group, true);
       }
     }
   }
