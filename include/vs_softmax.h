@@ -62,6 +62,8 @@ VS_API int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq,
  *   lse         [nq] fp32 as returned by vs_flat_logprob; entropy [nq] fp32 likewise, read if g_entropy is given.
  *   g_logp [nq, nt], g_lse [nq], g_entropy [nq]: fp32, each may be NULL (zeros); a target listed twice counts twice.
  *   out_dq [nq, d], out_dx [nb, d] of `dtype`, out_dbias [nb] fp32: each may be NULL (not wanted).
+ * A query whose g_logp, g_lse or g_entropy is infinite or NaN: NaN in its dq and in dx and dbias of the rows that exist.
+ * One for which all three are 0 takes no part, whatever it holds.
  * G is held in fp16 relative to a bound of its row (for fp32 vectors in two parts, together 22 bits), 2^-11 of a value
  * or 2^-38 of the bound; sums are fp32.
  * Errors: as vs_flat_logprob; entropy missing where g_entropy is given; VS_ERR_UNSUPPORTED beyond 2^23 tiles of 128 rows or

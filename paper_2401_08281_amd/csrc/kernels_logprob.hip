@@ -965,10 +965,12 @@ __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, in
   // |G| <= |c| p + |g_entropy| (p |logp| + p H) + sum |g_logp|, and p |logp| <= 1 / e
   const float top = fabsf(c) + mag + fabsf(ge) * (0.37f + fabsf(ent));
   int e = top > 0.f && top < __builtin_inff() ? (int)__builtin_amdgcn_frexp_expf(top) : 0;
-  e = e < -100 ? -100 : e;
-  // (infinite or NaN: so are the row's gradients; 0, a padded query: it takes no part, whatever it holds)
-  bound[i] = top == 0.f || !(top < __builtin_inff()) ? top : __builtin_ldexpf(1.f, e);
-  coef[i] = make_float4(c, ge, ent, top == 0.f ? neg_inf() : g.lse[i]);
+  e = e < -100 ? -100 : (e > 127 ? 127 : e);
+  // 0, a padded query: it takes no part, whatever it holds.  Infinite or NaN: G is NaN for the rows that exist (an infinite
+  // coefficient would leave infinities among them, and -inf marks a row that does not).
+  const bool bad = !(top < __builtin_inff());
+  bound[i] = top == 0.f || bad ? top : __builtin_ldexpf(1.f, e);
+  coef[i] = make_float4(bad ? __builtin_nanf("") : c, ge, ent, top == 0.f ? neg_inf() : g.lse[i]);
 }
 
 // Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
@@ -1138,11 +1140,13 @@ __device__ __forceinline__ void store_4(void* p, int64_t i, int n, bool whole, i
 // 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 141 us: 710 and 730 TFLOP/s.
 constexpr int kBigTile = 256;
 constexpr int kBigStage = 2 * kBigTile * 128;
-// With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type.
+// With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type, zeros
+// where row b does not exist (bias -inf): zeros of G may have met a query that is not finite.
 template <int PLANES, bool DIRECT>
 __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix B, int64_t kblocks, int splits, int add,
                                                             float* __restrict__ part, int64_t ld, int64_t ta, int64_t tb,
-                                                            const float* __restrict__ sa, float alpha, int dtype, int d) {
+                                                            const float* __restrict__ sa, float alpha, int dtype, int d,
+                                                            const float* __restrict__ bias) {
   extern __shared__ __align__(16) char lds[];
   int64_t ia, ib_;
   const int64_t tiles = ta * tb;
@@ -1221,6 +1225,7 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
     const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
     if (b >= B.rows) continue;
     if constexpr (DIRECT) {
+      const bool gone = bias && bias[b] == neg_inf();
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
@@ -1229,7 +1234,7 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
           if (a >= d) continue;
           float v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = a + u < d ? acc[ib][jb][r + u] * sa[a + u] * alpha : 0.f;
+          for (int u = 0; u < 4; ++u) v[u] = a + u < d && !gone ? acc[ib][jb][r + u] * sa[a + u] * alpha : 0.f;
           store_4(part, b * d + a, d - a, (d & 3) == 0, dtype, v);
         }
       continue;
@@ -1287,6 +1292,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void sm_product_out_kernel(const float* __restrict__ part, int splits, int64_t rows,
                                                              int64_t ld, int d, const float* __restrict__ sa,
                                                              const float* __restrict__ sb, float alpha,
+                                                             const float* __restrict__ bias,
                                                              typename Elem<DT>::T* __restrict__ out) {
   const int64_t i = group_id() * 256 + threadIdx.x;
   if (i >= rows * d) return;
@@ -1296,6 +1302,7 @@ __global__ __launch_bounds__(256) void sm_product_out_kernel(const float* __rest
   for (int s = 0; s < splits; ++s) v += part[(s * rows + b) * ld + a];
   // (powers of two first: the product with alpha is the only rounding before the last)
   v = v * sa[a] * (sb ? sb[b] : 1.f);
+  if (bias && bias[b] == neg_inf()) v = 0.f;              // (a row that does not exist: see sm_product_kernel)
   out[i] = (typename Elem<DT>::T)(v * alpha);
 }
 
@@ -1471,7 +1478,7 @@ void launch_sm_product(const SmForm& f, const SmProductPlan& pp, const SmMatrix&
     const unsigned g = (unsigned)(ta * tb * pp.splits);
     auto run = [&](auto kern) {
       (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBigStage);
-      kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb, nullptr, 0.f, 0, 0);
+      kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, pp.splits, add ? 1 : 0, part, ld, ta, tb, nullptr, 0.f, 0, 0, nullptr);
     };
     if (f.planes == 2) run(sm_product_kernel<2, false>);
     else run(sm_product_kernel<1, false>);
@@ -1484,23 +1491,23 @@ void launch_sm_product(const SmForm& f, const SmProductPlan& pp, const SmMatrix&
 }
 
 void launch_sm_product_direct(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, const float* sa,
-                              float alpha, int dtype, void* out, hipStream_t st) {
+                              float alpha, const float* bias, int dtype, void* out, hipStream_t st) {
   const int64_t ta = (A.rows + kBigTile - 1) / kBigTile, tb = (B.rows + kBigTile - 1) / kBigTile;
   const unsigned g = (unsigned)(ta * tb);
   auto run = [&](auto kern) {
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBigStage);
-    kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, 1, 0, static_cast<float*>(out), 0, ta, tb, sa, alpha, dtype, (int)A.rows);
+    kern<<<g, 512, 2 * kBigStage, st>>>(A, B, kblocks, 1, 0, static_cast<float*>(out), 0, ta, tb, sa, alpha, dtype, (int)A.rows, bias);
   };
   if (f.planes == 2) run(sm_product_kernel<2, true>);
   else run(sm_product_kernel<1, true>);
 }
 
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* sa, const float* sb,
-                           float alpha, int dtype, void* out, hipStream_t st) {
+                           float alpha, const float* bias, int dtype, void* out, hipStream_t st) {
   const dim3 g = grid_2d((rows * d + 255) / 256);
-  if (dtype == 0) sm_product_out_kernel<0><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<float*>(out));
-  else if (dtype == 1) sm_product_out_kernel<1><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<_Float16*>(out));
-  else sm_product_out_kernel<2><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, static_cast<__bf16*>(out));
+  if (dtype == 0) sm_product_out_kernel<0><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, bias, static_cast<float*>(out));
+  else if (dtype == 1) sm_product_out_kernel<1><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, bias, static_cast<_Float16*>(out));
+  else sm_product_out_kernel<2><<<g, 256, 0, st>>>(part, splits, rows, ld, d, sa, sb, alpha, bias, static_cast<__bf16*>(out));
 }
 
 void launch_sm_sum_parts(const float* part, int64_t n_parts, int64_t ld, int64_t n, float* out, hipStream_t st) {

@@ -98,12 +98,12 @@ struct SmProductPlan {
 SmProductPlan plan_sm_product(int64_t rows_a, int64_t rows_b, int64_t kblocks);
 void launch_sm_product(const SmForm& f, const SmProductPlan& p, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, bool add,
                        float* part, int64_t ld, hipStream_t st);
-// out[b][a] = alpha scale_a[a] sum_k A[a][k] B[b][k], in `dtype`
+// out[b][a] = alpha scale_a[a] sum_k A[a][k] B[b][k], in `dtype`; 0 where bias[b] is -inf (bias: or null)
 void launch_sm_product_direct(const SmForm& f, const SmMatrix& A, const SmMatrix& B, int64_t kblocks, const float* scale_a,
-                              float alpha, int dtype, void* out, hipStream_t st);
-// out[b][a] = alpha scale_a[a] scale_b[b] sum_split part[split][b][a]
+                              float alpha, const float* bias, int dtype, void* out, hipStream_t st);
+// out[b][a] = alpha scale_a[a] scale_b[b] sum_split part[split][b][a], likewise
 void launch_sm_product_out(const float* part, int splits, int64_t rows, int64_t ld, int d, const float* scale_a,
-                           const float* scale_b, float alpha, int dtype, void* out, hipStream_t st);
+                           const float* scale_b, float alpha, const float* bias, int dtype, void* out, hipStream_t st);
 void launch_sm_sum_parts(const float* part, int64_t n_parts, int64_t ld, int64_t n, float* out, hipStream_t st);
 void launch_sm_zero(void* p, int64_t bytes, hipStream_t st);
 

@@ -351,15 +351,15 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
       const SmMatrix a{ws + p.o_qt, p.qt_row, d, nullptr}, b{ws + p.o_gt, p.gt_row, n, nullptr};
       char* dx = static_cast<char*>(out_dx) + x0 * d * elem_bytes(dtype);
       if (p.to_x.big && p.to_x.splits == 1) {
-        launch_sm_product_direct(prod, a, b, p.f.blocks(nq), at(p.o_qts), alpha, dtype, dx, st);
+        launch_sm_product_direct(prod, a, b, p.f.blocks(nq), at(p.o_qts), alpha, s.bias, dtype, dx, st);
       } else {
         launch_sm_product(prod, p.to_x, a, b, p.f.blocks(nq), false, at(p.o_dx), p.ld, st);
-        launch_sm_product_out(at(p.o_dx), p.to_x.splits, n, p.ld, d, at(p.o_qts), nullptr, alpha, dtype, dx, st);
+        launch_sm_product_out(at(p.o_dx), p.to_x.splits, n, p.ld, d, at(p.o_qts), nullptr, alpha, s.bias, dtype, dx, st);
       }
     }
     if (out_dbias) launch_sm_sum_parts(at(p.o_db), (nq + p.tile_q - 1) / p.tile_q, p.chunk, n, out_dbias + x0, st);
   }
-  if (out_dq) launch_sm_product_out(at(p.o_dq), p.to_q.splits, nq, p.ld, d, at(p.o_xts), bound, alpha, dtype, out_dq, st);
+  if (out_dq) launch_sm_product_out(at(p.o_dq), p.to_q.splits, nq, p.ld, d, at(p.o_xts), bound, alpha, nullptr, dtype, out_dq, st);
   return launched(who);
 }
 
