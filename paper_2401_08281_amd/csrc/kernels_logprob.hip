@@ -210,9 +210,71 @@ __device__ __forceinline__ Best join_mixed(Best a, Best b) {
   return o;
 }
 
+// <x_a, q_b> of the vectors themselves
+__device__ __forceinline__ float raw_dot(const void* x, int64_t a, const void* q, int64_t b, int d, int dtype) {
+  float s = 0.f;
+  for (int k = 0; k < d; ++k) {
+    const int64_t i = a * d + k, j = b * d + k;
+    float u, v;
+    if (dtype == VS_FP32) { u = static_cast<const float*>(x)[i]; v = static_cast<const float*>(q)[j]; }
+    else if (dtype == VS_FP16) { u = (float)static_cast<const _Float16*>(x)[i]; v = (float)static_cast<const _Float16*>(q)[j]; }
+    else { u = (float)static_cast<const __bf16*>(x)[i]; v = (float)static_cast<const __bf16*>(q)[j]; }
+    s = __builtin_fmaf(u, v, s);
+  }
+  return s;
+}
+
+// The scores of rows and queries with an infinite component, once more from the vectors: a head and a tail cannot hold one
+// (its product with a tail of the other side has any sign), nor can a row be scaled by it.  A row, then a query at a time;
+// no workgroup without such a row or query comes here.
+template <int IB, int JB>
+__device__ __forceinline__ void infinite_scores(const SmScores& S, int64_t a0, int64_t b0, const float2* rowdata, f32x16 (&acc)[IB][JB]) {
+  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
+  float* patch = const_cast<float*>(reinterpret_cast<const float*>(rowdata + 64 * IB)) + 4;       // [64 max(IB, JB)]
+#pragma unroll 1
+  for (int i = 0; i < 64 * IB; ++i) {
+    const float2 rd = rowdata[i];                                        // (the same for all)
+    if (rd.x < __builtin_inff() || rd.y == neg_inf()) continue;
+    __syncthreads();
+    if (threadIdx.x < 64 * JB && b0 + threadIdx.x < S.nq)
+      patch[threadIdx.x] = raw_dot(S.raw_x, a0 + i, S.raw_q, b0 + threadIdx.x, S.d, S.dtype) * S.scale + rd.y;
+    __syncthreads();
+    float s[JB];
+#pragma unroll
+    for (int jb = 0; jb < JB; ++jb) s[jb] = patch[(wb * JB + jb) * 32 + (lane & 31)];
+    const int mine = i - wa * 32 * IB - 4 * half;
+#pragma unroll
+    for (int ib = 0; ib < IB; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) acc[ib][jb][r] = mine == ib * 32 + (r & 3) + 8 * (r >> 2) ? s[jb] : acc[ib][jb][r];
+  }
+#pragma unroll 1
+  for (int c = 0; c < 64 * JB; ++c) {
+    if (b0 + c >= S.nq || S.q.scale[b0 + c] < __builtin_inff()) continue;
+    __syncthreads();
+    if (threadIdx.x < 64 * IB) {
+      const float b = rowdata[threadIdx.x].y;
+      patch[threadIdx.x] = b == neg_inf() ? neg_inf() : raw_dot(S.raw_x, a0 + threadIdx.x, S.raw_q, b0 + c, S.d, S.dtype) * S.scale + b;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ib = 0; ib < IB; ++ib)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float s = patch[(wa * IB + ib) * 32 + (r & 3) + 8 * (r >> 2) + 4 * half];
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+          if ((wb * JB + jb) * 32 + (lane & 31) == c) acc[ib][jb][r] = s;
+      }
+  }
+  __syncthreads();
+}
+
 // The scores of a wavefront's tile in place of its products: s = acc * (row factor * query factor) + bias, -inf for
 // rows that do not exist (past the end, or bias -inf: whatever their products are).
-// rowdata: LDS, {row factor, bias} of the workgroup's 256 rows, filled here.
+// rowdata: LDS, {row factor, bias} of the workgroup's rows, filled here.
 template <int IB, int JB>
 __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[IB][JB]) {
   const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1;
@@ -220,7 +282,19 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
   if (!plain) {
     const int64_t j = a0 + threadIdx.x;
     const bool in = j < S.nx;
-    if (threadIdx.x < 64 * IB) rowdata[threadIdx.x] = make_float2(in && S.x.scale ? S.x.scale[j] : 1.f, in ? (S.bias ? S.bias[j] : 0.f) : neg_inf());
+    float xs = 1.f, qs = 1.f, b = neg_inf();
+    if (in) {
+      if (S.x.scale) xs = S.x.scale[j];
+      b = S.bias ? S.bias[j] : 0.f;
+    }
+    if (threadIdx.x < 64 * IB) rowdata[threadIdx.x] = make_float2(xs, b);
+    // (whether an infinite component takes part: a word of every wavefront)
+    if (S.raw_x) {
+      if (threadIdx.x < 64 * JB && b0 + threadIdx.x < S.nq) qs = S.q.scale[b0 + threadIdx.x];
+      const bool odd = (threadIdx.x < 64 * IB && b != neg_inf() && !(xs < __builtin_inff())) || !(qs < __builtin_inff());
+      const u64 any = __ballot(odd);
+      if (lane == 0) reinterpret_cast<u32*>(rowdata + 64 * IB)[wave] = any != 0 ? 1u : 0u;
+    }
     __syncthreads();
   }
   float cq[JB];
@@ -245,6 +319,10 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
         }
       }
     }
+  if (!plain && S.raw_x) {
+    const u32x4 odd = *reinterpret_cast<const u32x4*>(rowdata + 64 * IB);
+    if (__builtin_amdgcn_readfirstlane(odd[0] | odd[1] | odd[2] | odd[3]) != 0) infinite_scores(S, a0, b0, rowdata, acc);
+  }
 }
 
 // ---- forward: scores -> softmax records ---------------------------------------------
@@ -818,7 +896,7 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide 
       put(k, v[0]);
     }
   }
-  if (l == 0) scale[r] = down;
+  if (l == 0) scale[r] = mx < __builtin_inff() ? down : mx;             // (see infinite_scores)
 }
 
 // Largest size in every column: a thread goes down 16 bytes of columns, four rows in flight, as many rows beside each

@@ -42,7 +42,7 @@ struct SmSide {
   const float* bias = nullptr;      // rows whose bias is -inf become zeros
   const float* factor = nullptr;    // of every row, for its columns; a row of factor 0 is not read
   void* rows = nullptr;             // out: every row as K blocks of fp16 parts times 1 / row_scale, its largest component in
-  float* row_scale = nullptr;       // [128, 256)
+  float* row_scale = nullptr;       // [128, 256); infinite for a row with an infinite component
   void* cols = nullptr;             // out: every column of (factor x) as K blocks over the rows, likewise
   float* col_scale = nullptr;
   u32* colmax = nullptr;            // [d] of scratch, zeros on entry
@@ -57,6 +57,9 @@ struct SmScores {                   // s = scale <q, x> + bias for rows x0 .. x0
   int64_t nx = 0, nq = 0;
   const float* bias = nullptr;      // of these rows
   float scale = 1.f;
+  const void* raw_x = nullptr;      // the vectors themselves, where x and q are prepared copies
+  const void* raw_q = nullptr;
+  int d = 0, dtype = 0;
 };
 struct SmRecords {                  // softmax of 128 rows: {max, sum, sum e (s - max), second best | position of the max}
   float4* rec = nullptr;            // [nq, parts]

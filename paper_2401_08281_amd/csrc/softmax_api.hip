@@ -248,6 +248,7 @@ int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq, int32_
     launch_sm_prep_rows(p.f, sx, sq, d, st);
     s.x = SmMatrix{sx.rows, p.row_bytes, nb, sx.row_scale};
     s.q = SmMatrix{sq.rows, p.row_bytes, nq, sq.row_scale};
+    s.raw_x = x; s.d = d; s.dtype = dtype;
   }
   SmRecords r;
   r.rec = reinterpret_cast<float4*>(ws + p.o_rec);
@@ -264,6 +265,7 @@ int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq, int32_
       } else {
         s.q = SmMatrix{static_cast<const char*>(qs.p) + q0 * qs.row_bytes, qs.row_bytes, n, qs.scale ? qs.scale + q0 : nullptr};
         s.nq = n;
+        s.raw_q = qp;
         launch_sm_scores(p.f, p.direct, s, r, k > 0 && !p.keep, st);
       }
     }
@@ -328,6 +330,7 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     launch_sm_prep_rows(p.f, sx, sq, d, st);
     xp = ws + p.o_x; xs = at(p.o_xs);
     s.q = SmMatrix{sq.rows, p.row_bytes, nq, sq.row_scale};
+    s.raw_q = q; s.d = d; s.dtype = dtype;
   }
   SmSide cx = sx, cq = sq;
   if (!out_dq) cx.n = 0;
@@ -338,6 +341,7 @@ int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_t nq, i
     const int64_t n = std::min(p.chunk, nb - x0);
     s.x = SmMatrix{xp + x0 * p.row_bytes, p.row_bytes, n, xs ? xs + x0 : nullptr};
     s.nx = n;
+    if (!p.direct) s.raw_x = static_cast<const char*>(x) + x0 * d * elem_bytes(dtype);
     s.bias = bias ? bias + x0 : nullptr;
     SmGOut o{reinterpret_cast<float4*>(ws + p.o_coef), bound, targets, nt, g.g_logp, x0,
              out_dq ? ws + p.o_g : nullptr, p.g_row, out_dx ? ws + p.o_gt : nullptr, p.gt_row,
