@@ -40,9 +40,11 @@ enum { VS_FP32 = 0, VS_FP16 = 1, VS_BF16 = 2 };
  *   out_top_logp, out_top_ids [nq, k] fp32, int64: the k largest log-probabilities and their rows, best first,
  *               ties to the smaller row; slots without a row: -inf and -1.  k = 0: none (NULL).
  * A query without any row (nb = 0, or every bias -inf): lse -inf, entropy 0, logp -inf, no alternatives.
- * Scores are fp32 sums of products that are exact for fp16 and bf16 rows; fp32 rows go as two fp16 parts
- * each, relative to the largest component of their row, and lose at most 2^-21 |q||x| of a score that way (up to 64
- * queries they are multiplied in fp32).  Order among scores closer than their rounding may differ from the exact one.
+ * A score of +inf or NaN makes its query's lse, entropy and log-probabilities NaN.
+ * Scores are fp32 sums of products; these are exact (fp32: rounded) up to 64 queries and for fp16 and bf16 rows of a multiple
+ * of 64 components.  Otherwise rows are multiplied from copies relative to the largest component of their row: 16-bit components lose at most 2^-39 of it (nothing above 2^-31 of it); fp32 ones, two fp16 parts each, at most 2^-24
+ * of themselves or 2^-39 of it, and a score at most 2^-21 |q||x| that way.  Order among scores closer than their rounding
+ * may differ from the exact one; rows that are equal go by number.
  * Errors: null pointers (with nq > 0), d outside [1, VS_MAX_ROW], nb or nq outside [0, 2^31), nt < 0, k outside [0, VS_MAX_TOP], unknown
  * dtype, scale not finite, misaligned vectors or work space, a work space that is too small.  nq = 0 is a no-op.
  */
@@ -64,8 +66,11 @@ VS_API int vs_flat_logprob(const void* x, int64_t nb, const void* q, int64_t nq,
  *   out_dq [nq, d], out_dx [nb, d] of `dtype`, out_dbias [nb] fp32: each may be NULL (not wanted).
  * A query whose g_logp, g_lse or g_entropy is infinite or NaN: NaN in its dq and in dx and dbias of the rows that exist.
  * One for which all three are 0 takes no part, whatever it holds.
- * G is held in fp16 relative to a bound of its row (for fp32 vectors in two parts, together 22 bits), 2^-11 of a value
- * or 2^-38 of the bound; sums are fp32.
+ * The scores are computed as vs_flat_logprob does beyond 64 queries.  G is held in fp16 relative to a bound of its row (for
+ * fp32 vectors in two parts, together 22 bits), 2^-11 of a value or 2^-38 of the bound.  The vectors that it multiplies are
+ * held likewise, relative to the largest component of their column: column t of dq with x_jt over the rows that exist, column
+ * t of dx with bound_i q_it over the queries; 2^-24 (fp32) or nothing (16 bits) of a component is lost, and at most 2^-39 of that
+ * largest one.  Sums are fp32.
  * Errors: as vs_flat_logprob; entropy missing where g_entropy is given; VS_ERR_UNSUPPORTED beyond 2^23 tiles of 128 rows or
  * components by 64 queries.  nq = 0 sets out_dx and out_dbias to zero.
  */

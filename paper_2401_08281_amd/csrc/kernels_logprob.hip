@@ -284,7 +284,7 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
     const bool in = j < S.nx;
     float xs = 1.f, qs = 1.f, b = neg_inf();
     if (in) {
-      if (S.x.scale) xs = S.x.scale[j];
+      if (S.x.scale) xs = S.x.scale[j] * 0x1p-14f;             // (prepared queries are up to 2^15: 2^14 goes over to their factor)
       b = S.bias ? S.bias[j] : 0.f;
     }
     if (threadIdx.x < 64 * IB) rowdata[threadIdx.x] = make_float2(xs, b);
@@ -301,7 +301,7 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) {
     const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
-    cq[jb] = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] : 1.f);
+    cq[jb] = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] * 0x1p14f : 1.f);
   }
 #pragma unroll
   for (int ib = 0; ib < IB; ++ib)
@@ -803,10 +803,11 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
 }
 
 // ---- preparation of operands ------------------------------------------------------------
-// The power of two that brings a largest component of `mx` into [128, 256); what lies 2^22 below it still has its head's
-// full 11 bits, and a tail keeps 2^-32 of the largest component.
+// The power of two that brings a largest component of `mx` into [2^14, 2^15), the top of fp16's range: what lies 2^28 below
+// it still has its head's full 11 bits, and half a step of the smallest numbers, 2^-25, is 2^-39 of the largest component.
+// A head and a tail together keep 2^-24 of a component, as fp32 does, down to 2^-15 of the largest.
 __device__ __forceinline__ void row_scale(float mx, float* up, float* down) {
-  int e = mx > 0.f && mx < __builtin_inff() ? 8 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
+  int e = mx > 0.f && mx < __builtin_inff() ? 15 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
   e = e < -120 ? -120 : (e > 120 ? 120 : e);
   *up = __builtin_ldexpf(1.f, e);
   *down = __builtin_ldexpf(1.f, -e);
