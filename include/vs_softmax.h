@@ -42,9 +42,10 @@ enum { VS_FP32 = 0, VS_FP16 = 1, VS_BF16 = 2 };
  * A query without any row (nb = 0, or every bias -inf): lse -inf, entropy 0, logp -inf, no alternatives.
  * A score of +inf or NaN makes its query's lse, entropy and log-probabilities NaN.
  * Scores are fp32 sums of products; these are exact (fp32: rounded) up to 64 queries and for fp16 and bf16 rows of a multiple
- * of 64 components.  Otherwise rows are multiplied from copies relative to the largest component of their row: 16-bit components lose at most 2^-39 of it (nothing above 2^-31 of it); fp32 ones, two fp16 parts each, at most 2^-24
- * of themselves or 2^-39 of it, and a score at most 2^-21 |q||x| that way.  Order among scores closer than their rounding
- * may differ from the exact one; rows that are equal go by number.
+ * of 64 components.  Otherwise rows are multiplied from copies relative to the largest component of their row: 16-bit
+ * components lose at most 2^-39 of it (nothing above 2^-31 of it); fp32 ones, two fp16 parts each, at most 2^-24 of themselves
+ * or 2^-39 of it, and a score at most 2^-21 |q||x| that way.  Order among scores closer than their rounding may differ from
+ * the exact one; rows that are equal go by number.
  * Errors: null pointers (with nq > 0), d outside [1, VS_MAX_ROW], nb or nq outside [0, 2^31), nt < 0, k outside [0, VS_MAX_TOP], unknown
  * dtype, scale not finite, misaligned vectors or work space, a work space that is too small.  nq = 0 is a no-op.
  */
@@ -91,6 +92,10 @@ VS_API int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_
  *            with zeros behind its dk components (all lists where nprobe >= nlist).
  *   limits   [nq] int64 or NULL: query i sees the vectors whose id is below limits[i] (positions up to its own).
  *   out      [nq, d - v0] of `dtype`, out_lse [nq] fp32 (may be NULL).  A query that sees nothing: zeros and -inf.
+ * Scores, weights and sums are fp32, in one of two forms by the size of the call: sums of look-ups in fp32 tables, or, for many
+ * queries over all lists, products of fp16 parts of codewords and queries.  These keep 2^-24 of a component or 2^-39 of the
+ * largest codeword in it (components more than 2^24 smaller than the largest one: 2^-63 of that), as long as the centroids are
+ * less than 2^40 of it; the weights are then held in 22 bits, for fp16 and bf16 queries in 11.
  * The index is not written.  With 0 < nprobe < nlist the coarse quantizer uses the index's own work space, as
  * vs_ivfpq_search does: such calls on one index must not overlap in time, the first of a size allocates, and a stream under
  * capture is refused (VS_ERR_UNSUPPORTED).

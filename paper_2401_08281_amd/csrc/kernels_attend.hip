@@ -682,8 +682,11 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
 //   product O^T = V^T p^T: a wavefront takes 16 components of every 64 (operand A: lane = component, 8 rows a step,
 //           looked up one by one in a table [component][16]).
 // The centroid of a list adds a constant to its scores and sum(p) centroid to the product, both once per list and part.
-// The tables are relative to a power of two each and keep head and tail (22 bits), so scores are good to fp32; weights
-// keep 11 bits for 16-bit queries, whose results have no more, and 22 for fp32.
+// Every component has a power of two of its own, which brings its largest codeword to [2^14, 2^15), the top of fp16's range:
+// tables hold its codewords times that, queries its value over it (and times a power of two of the query that brings the
+// largest of these there), results are taken back by it at the end.  So head and tail keep 2^-24 of a codeword or 2^-39 of its
+// component's largest, whatever the sizes of other components, and scores are good to fp32; 16-bit queries are exact down to
+// 2^-31 of the largest such value.  Weights keep 11 bits for 16-bit queries, whose results have no more, and 22 for fp32.
 // The gradient's tile computes p from lse and the product of g with the values, w = p <g, t> and adds w k and p k; both
 // relative to the centroid part of <g, v> of the present list, which is exchanged when the list changes.
 // Bound by nothing alone: of a tile's time the score products, the weighted products, the staging of codes and the maxima
@@ -710,7 +713,7 @@ __host__ __device__ inline CodeSet code_set(int m0, int n, int dsub, int w) {
   return c;
 }
 struct TileLds {                               // bytes
-  int ktab, gtab, vtab, qf, gf, krow, grow, vcol, p, ids, red, stat, cent, total;
+  int ktab, gtab, vtab, qf, gf, krow, grow, vcol, p, ids, red, stat, cent, exps, total;
   int p_stride, p_set, stage;
 };
 // 64-component runs of the result that a tile kernel is made for
@@ -737,8 +740,9 @@ __host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, 
   o.p_set = planes * nq * 16 * o.p_stride;
   o.p = take((grad ? 2 : 1) * o.p_set);
   o.red = take(4 * 2 * nq * 16 * 4);
-  o.stat = take(nq * 16 * 6 * 4);
+  o.stat = take(nq * 16 * 3 * 4);
   o.cent = take((dk + dv) * 4);
+  o.exps = take((dk + dv) * 4);
   o.total = at;
   return o;
 }
@@ -749,6 +753,11 @@ __device__ __forceinline__ void unit_scale(float mx, float* up, float* down) {
   e = e < -120 ? -120 : (e > 120 ? 120 : e);
   *up = __builtin_ldexpf(1.f, e);
   *down = __builtin_ldexpf(1.f, -e);
+}
+// The exponent of the power of two that brings `mx` into [2^14, 2^15)
+__device__ __forceinline__ int top_exponent(float mx) {
+  const int e = mx > 0.f && mx < __builtin_inff() ? 15 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
+  return e < -126 ? -126 : (e > 126 ? 126 : e);
 }
 __device__ __forceinline__ u32 pack_parts(float v) {     // {head, tail}
   const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
@@ -769,9 +778,10 @@ __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Table of a code set: piece (j, code) of codeword c at ((j 4 mq + code) 16 + c) entry bytes, {W heads, W tails}.
+// Table of a code set: piece (j, code) of codeword c at ((j 4 mq + code) 16 + c) entry bytes, {W heads, W tails}, times 2 to
+// the exponents of the set's components.
 template <int W>
-__device__ __forceinline__ void build_rows_table(char* tab, const CodeSet& c, const float* codebooks, int dsub, float up) {
+__device__ __forceinline__ void build_rows_table(char* tab, const CodeSet& c, const float* codebooks, int dsub, const int* exps) {
   const int n = c.ppc * 4 * c.mq * 16;
   for (int i = threadIdx.x; i < n; i += 256) {
     const int w = i & 15, jc = i >> 4, code = jc % (4 * c.mq), j = jc / (4 * c.mq);
@@ -779,7 +789,7 @@ __device__ __forceinline__ void build_rows_table(char* tab, const CodeSet& c, co
 #pragma unroll
     for (int t = 0; t < W; ++t) {
       const int u = j * W + t;
-      const float v = code < c.n && u < dsub ? codebooks[((int64_t)(c.m0 + code) * 16 + w) * dsub + u] * up : 0.f;
+      const float v = code < c.n && u < dsub ? __builtin_ldexpf(codebooks[((int64_t)(c.m0 + code) * 16 + w) * dsub + u], exps[code * dsub + u]) : 0.f;
       const _Float16 hi = (_Float16)v;
       e[t] = hi;
       e[W + t] = (_Float16)(v - (float)hi);
@@ -826,16 +836,17 @@ __device__ __forceinline__ const void* row_of(const void* p, int64_t row, int ld
   return static_cast<const char*>(p) + row * ld * (dtype == VS_FP32 ? 4 : 2);
 }
 // Operand B of a code set, [plane][block of 16][step][64 lanes]: the lane of query ql and group g holds its share in the
-// order of the steps, times up.  (The fragments hold zeros before.)
+// order of the steps, times 2 to e less its component's exponent.  (The fragments hold zeros before.)
 template <int W, int PL>
 __device__ __forceinline__ void put_query_fragments(char* out, const CodeSet& c, int nqb, int ql, int g, const void* row,
-                                                    int dtype, int dsub, float up) {
+                                                    int dtype, int dsub, const int* exps, int e) {
   constexpr int PER = 8 / W;
   const int plane = nqb * c.steps * 1024, per_j = c.mq / PER;
   char* lane_at = out + ((ql >> 4) * c.steps * 64 + g * 16 + (ql & 15)) * 16;
   int code = 0, u = 0;                         // of the component that comes next
-  each_component(row, share_of(c, g, dsub), dtype, [&](int, float x) {
-    const float v = x * up;
+  const Share sh = share_of(c, g, dsub);
+  each_component(row, sh, dtype, [&](int i, float x) {
+    const float v = __builtin_ldexpf(x, e - exps[sh.t0 + i]);
     const _Float16 hi = (_Float16)v;
     const int step = u / W * per_j + code / PER, t = code % PER * W + u % W;
     _Float16* at = reinterpret_cast<_Float16*>(lane_at + step * 1024) + t;
@@ -917,27 +928,49 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   if (q0 >= A.nq) return;
   const int64_t r0 = split * A.per, r1 = r0 + A.per < A.ntotal ? r0 + A.per : A.ntotal;
   float* red = reinterpret_cast<float*>(ldsb + L.red);
-  float* stat = reinterpret_cast<float*>(ldsb + L.stat);     // per query: up, down of q; up, down of g; bound of w; bias
+  float* stat = reinterpret_cast<float*>(ldsb + L.stat);     // per query: factor of its products, of those of g; bound of w
   float* cent = reinterpret_cast<float*>(ldsb + L.cent);     // centroid of the list: [dk] keys, [dv] values
 
-  // scales: of the key and value codewords, and of every query
-  float km = 0.f, vm = 0.f;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < mk * 16 * dsub; i += 256) km = fmaxf(km, fabsf(A.codebooks[i]));
-#pragma unroll 8
-  for (int i = threadIdx.x; i < mv * 16 * dsub; i += 256) vm = fmaxf(vm, fabsf(A.codebooks[(int64_t)mv0 * 16 * dsub + i]));
+  // exponents of the key and value components (zeros take the largest one), then factors of every query
+  int* kexp = reinterpret_cast<int*>(ldsb + L.exps);
+  int* vexp = kexp + A.dk;
+  constexpr int kNone = 1 << 20;
+  int kmin = kNone, vmin = kNone;
+  for (int t = threadIdx.x; t < A.dk + dv; t += 256) {
+    const int comp = t < A.dk ? t : A.v0 + t - A.dk, m = comp / dsub;
+    const float* cb = A.codebooks + (int64_t)m * 16 * dsub + (comp - m * dsub);
+    float mx = 0.f;
+#pragma unroll
+    for (int c = 0; c < 16; ++c) mx = fmaxf(mx, fabsf(cb[c * dsub]));
+    const int e = mx > 0.f ? top_exponent(mx) : kNone;
+    kexp[t] = e;
+    if (t < A.dk) kmin = e < kmin ? e : kmin;
+    else vmin = e < vmin ? e : vmin;
+  }
   for (int i = threadIdx.x; i < PL * NQ * K.steps * 64; i += 256) reinterpret_cast<u32x4*>(ldsb + L.qf)[i] = u32x4{0, 0, 0, 0};
   if (GRAD)
     for (int i = threadIdx.x; i < PL * NQ * V.steps * 64; i += 256) reinterpret_cast<u32x4*>(ldsb + L.gf)[i] = u32x4{0, 0, 0, 0};
-  km = wave_max(km);
-  vm = wave_max(vm);
-  if (lane == 0) { red[wave] = km; red[4 + wave] = vm; }
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) {
+    const int a = __shfl_xor(kmin, w), b = __shfl_xor(vmin, w);
+    kmin = a < kmin ? a : kmin;
+    vmin = b < vmin ? b : vmin;
+  }
+  if (lane == 0) { reinterpret_cast<int*>(red)[wave] = kmin; reinterpret_cast<int*>(red)[4 + wave] = vmin; }
   __syncthreads();
-  km = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  vm = fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7]));
-  float k_up, k_down, v_up, v_down;
-  unit_scale(km, &k_up, &k_down);
-  unit_scale(vm, &v_up, &v_down);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int a = reinterpret_cast<int*>(red)[w], b = reinterpret_cast<int*>(red)[4 + w];
+    kmin = a < kmin ? a : kmin;
+    vmin = b < vmin ? b : vmin;
+  }
+  // No more than 24 above the smallest: sums hold centroids as well, times the same power, and 24 more bits of range are what
+  // parts of smaller components have anyway.
+  for (int t = threadIdx.x; t < A.dk + dv; t += 256) {
+    const int low = t < A.dk ? kmin : vmin, most = (low == kNone ? 0 : low) + 24;
+    kexp[t] = kexp[t] < most ? kexp[t] : most;
+  }
+  __syncthreads();
   // four threads a query, a lane group's share of the components each
   const int ql = threadIdx.x >> 2, qg = threadIdx.x & 3;
   const bool q_thread = ql < QT;
@@ -945,32 +978,37 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
   const void* g_row = GRAD && q_row ? row_of(A.g_out, q0 + ql, dv, A.dtype) : nullptr;
   if (q_thread) {
     float mx = 0.f, gx = 0.f, g1 = 0.f;
-    if (q_row) each_component(q_row, share_of(K, qg, dsub), A.dtype, [&](int, float v) { mx = fmaxf(mx, fabsf(v)); });
-    if (g_row) each_component(g_row, share_of(V, qg, dsub), A.dtype, [&](int, float v) { gx = fmaxf(gx, fabsf(v)); g1 += fabsf(v); });
+    const Share ks = share_of(K, qg, dsub), vs = share_of(V, qg, dsub);
+    if (q_row) each_component(q_row, ks, A.dtype, [&](int i, float v) { mx = fmaxf(mx, __builtin_ldexpf(fabsf(v), -kexp[ks.t0 + i])); });
+    if (g_row)
+      each_component(g_row, vs, A.dtype, [&](int i, float v) {
+        const float w = __builtin_ldexpf(fabsf(v), -vexp[vs.t0 + i]);
+        gx = fmaxf(gx, w);
+        g1 += w;
+      });
 #pragma unroll
     for (int w = 1; w < 4; w <<= 1) {
       mx = fmaxf(mx, __shfl_xor(mx, w));
       if (GRAD) { gx = fmaxf(gx, __shfl_xor(gx, w)); g1 += __shfl_xor(g1, w); }
     }
-    float up, down;
-    unit_scale(mx, &up, &down);
-    if (qg == 0) { stat[ql] = up; stat[QT + ql] = down; }
-    if (q_row) put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, up);
+    const int e = top_exponent(mx);
+    if (qg == 0) stat[ql] = __builtin_ldexpf(1.f, -e);
+    if (q_row) put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, kexp, e);
     if (GRAD) {
-      float gup, gdown, bup, bdown;
-      unit_scale(gx, &gup, &gdown);
-      unit_scale(g1 * vm, &bup, &bdown);                     // |<g, t>| <= |g|_1 max |t| < 2 bdown
-      if (qg == 0) { stat[2 * QT + ql] = gup; stat[3 * QT + ql] = gdown; stat[4 * QT + ql] = bdown; }
-      if (g_row) put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, gup);
+      const int ge = top_exponent(gx);
+      float bup, bdown;
+      unit_scale(g1 * 32768.f, &bup, &bdown);                // |<g, t>| <= sum |g_t| max |t| < 2 bdown
+      if (qg == 0) { stat[QT + ql] = __builtin_ldexpf(1.f, -ge); stat[2 * QT + ql] = bdown; }
+      if (g_row) put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, vexp, ge);
     }
   }
   __syncthreads();
-  build_rows_table<W>(ldsb + L.ktab, K, A.codebooks, dsub, k_up);
-  if (GRAD) build_rows_table<W>(ldsb + L.gtab, V, A.codebooks, dsub, v_up);
-  const float o_up = GRAD ? k_up : v_up, o_down = GRAD ? k_down : v_down;
+  build_rows_table<W>(ldsb + L.ktab, K, A.codebooks, dsub, kexp);
+  if (GRAD) build_rows_table<W>(ldsb + L.gtab, V, A.codebooks, dsub, vexp);
+  const int* oexp = GRAD ? kexp : vexp;                      // of the results' components
   for (int i = threadIdx.x; i < NB * 64 * 16; i += 256) {
     const int t = i >> 4, c = i & 15, m = t / dsub;
-    reinterpret_cast<u32*>(ldsb + L.vtab)[i] = t < nout ? pack_parts(A.codebooks[((int64_t)(om0 + m) * 16 + c) * dsub + t - m * dsub] * o_up) : 0u;
+    reinterpret_cast<u32*>(ldsb + L.vtab)[i] = t < nout ? pack_parts(__builtin_ldexpf(A.codebooks[((int64_t)(om0 + m) * 16 + c) * dsub + t - m * dsub], oexp[t])) : 0u;
   }
   __syncthreads();
 
@@ -986,9 +1024,9 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     lse[qb] = GRAD && in ? A.lse[qi] * kLog2e : 0.f;
     if (GRAD && lse[qb] == neg_inf()) limit[qb] = INT64_MIN;
     all_in = all_in && limit[qb] != INT64_MIN;
-    fs[qb] = A.scale * (k_down * stat[QT + qb * 16 + col]) * kLog2e;     // (scores in units of log 2 inside)
-    fg[qb] = GRAD ? v_down * stat[3 * QT + qb * 16 + col] : 0.f;
-    fw[qb] = GRAD ? 1.f / stat[4 * QT + qb * 16 + col] : 0.f;
+    fs[qb] = A.scale * stat[qb * 16 + col] * kLog2e;         // (scores in units of log 2 inside)
+    fg[qb] = GRAD ? stat[QT + qb * 16 + col] : 0.f;
+    fw[qb] = GRAD ? 1.f / stat[2 * QT + qb * 16 + col] : 0.f;
     mx[qb] = neg_inf(); lp[qb] = 0.f; lw[qb] = 0.f; sum[qb] = 0.f; sum2[qb] = 0.f; bias[qb] = 0.f;
     seen_to = limit[qb] > seen_to ? limit[qb] : seen_to;
   }
@@ -1024,16 +1062,16 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       float p = 0.f, w = 0.f;
 #pragma unroll
       for (int v = 0; v < 4; ++v) { p += red[(v * 2) * QT + qb * 16 + col]; if (GRAD) w += red[(v * 2 + 1) * QT + qb * 16 + col]; }
-      sum[qb] += p;                              // (sums times 2^14; o also times o_up, and w over its bound)
+      sum[qb] += p;                              // (sums times 2^14; o also times its component's power, and w over its bound)
       sum2[qb] += w;
-      const float ps = p * o_up, ws = GRAD ? w * fw[qb] * o_up : 0.f;
+      const float ws = GRAD ? w * fw[qb] : 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int t = (nb * 4 + wave) * 16 + 4 * g + r;
-          const float cv = t < nout ? c[t] : 0.f;
-          o[SETS - 1][nb][qb][r] = __builtin_fmaf(cv, ps, o[SETS - 1][nb][qb][r]);
+          const float cv = t < nout ? __builtin_ldexpf(c[t], oexp[t]) : 0.f;
+          o[SETS - 1][nb][qb][r] = __builtin_fmaf(cv, p, o[SETS - 1][nb][qb][r]);
           if (GRAD) o[0][nb][qb][r] = __builtin_fmaf(cv, ws, o[0][nb][qb][r]);
         }
     }
@@ -1302,7 +1340,6 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     const int64_t qi = q0 + qb * 16 + col;
     if (qi >= A.nq) continue;
     float* out = A.part + (qi * A.nsplit + split) * A.ld;
-    const float f = o_down * (1.f / (float)(1 << kTableBits));
     if (wave == 0 && g == 0) {
       constexpr float one = 1.f / (float)(1 << kTableBits);
       out[0] = GRAD ? sum2[qb] * one : mx[qb] * kLn2;
@@ -1315,11 +1352,12 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       for (int r = 0; r < 4; ++r) {
         const int t = (nb * 4 + wave) * 16 + 4 * g + r;
         if (t >= nout) continue;
+        const int e = -kTableBits - oexp[t];
         if (GRAD) {
-          out[3 + t] = o[0][nb][qb][r] * (f * stat[4 * QT + qb * 16 + col]);
-          out[3 + nout + t] = o[SETS - 1][nb][qb][r] * f;
+          out[3 + t] = __builtin_ldexpf(o[0][nb][qb][r], e) * stat[2 * QT + qb * 16 + col];
+          out[3 + nout + t] = __builtin_ldexpf(o[SETS - 1][nb][qb][r], e);
         } else {
-          out[2 + t] = o[0][nb][qb][r] * f;
+          out[2 + t] = __builtin_ldexpf(o[0][nb][qb][r], e);
         }
       }
   }
