@@ -279,29 +279,31 @@ template <int IB, int JB>
 __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[IB][JB]) {
   const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1;
   const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + 64 * IB <= S.nx;   // (the same in the workgroup)
+  float cq[JB];
+  bool odd = false;                                                      // an infinite component takes part
+#pragma unroll
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
+    cq[jb] = S.q.scale && qi < S.nq ? S.q.scale[qi] * 0x1p14f : 1.f;
+    odd = odd || !(cq[jb] < __builtin_inff());
+    cq[jb] *= S.scale;
+  }
   if (!plain) {
     const int64_t j = a0 + threadIdx.x;
-    const bool in = j < S.nx;
-    float xs = 1.f, qs = 1.f, b = neg_inf();
-    if (in) {
-      if (S.x.scale) xs = S.x.scale[j] * 0x1p-14f;             // (prepared queries are up to 2^15: 2^14 goes over to their factor)
-      b = S.bias ? S.bias[j] : 0.f;
+    if (threadIdx.x < 64 * IB) {
+      float xs = 1.f, b = neg_inf();
+      if (j < S.nx) {
+        if (S.x.scale) xs = S.x.scale[j] * 0x1p-14f;           // (prepared queries are up to 2^15: 2^14 goes over to their factor)
+        b = S.bias ? S.bias[j] : 0.f;
+      }
+      rowdata[threadIdx.x] = make_float2(xs, b);
+      odd = odd || (b != neg_inf() && !(xs < __builtin_inff()));
     }
-    if (threadIdx.x < 64 * IB) rowdata[threadIdx.x] = make_float2(xs, b);
-    // (whether an infinite component takes part: a word of every wavefront)
-    if (S.raw_x) {
-      if (threadIdx.x < 64 * JB && b0 + threadIdx.x < S.nq) qs = S.q.scale[b0 + threadIdx.x];
-      const bool odd = (threadIdx.x < 64 * IB && b != neg_inf() && !(xs < __builtin_inff())) || !(qs < __builtin_inff());
+    if (S.raw_x) {                                             // (a word of every wavefront)
       const u64 any = __ballot(odd);
       if (lane == 0) reinterpret_cast<u32*>(rowdata + 64 * IB)[wave] = any != 0 ? 1u : 0u;
     }
     __syncthreads();
-  }
-  float cq[JB];
-#pragma unroll
-  for (int jb = 0; jb < JB; ++jb) {
-    const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
-    cq[jb] = S.scale * (S.q.scale && qi < S.nq ? S.q.scale[qi] * 0x1p14f : 1.f);
   }
 #pragma unroll
   for (int ib = 0; ib < IB; ++ib)
@@ -320,8 +322,8 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
       }
     }
   if (!plain && S.raw_x) {
-    const u32x4 odd = *reinterpret_cast<const u32x4*>(rowdata + 64 * IB);
-    if (__builtin_amdgcn_readfirstlane(odd[0] | odd[1] | odd[2] | odd[3]) != 0) infinite_scores(S, a0, b0, rowdata, acc);
+    const u32x4 any = *reinterpret_cast<const u32x4*>(rowdata + 64 * IB);
+    if (__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]) != 0) infinite_scores(S, a0, b0, rowdata, acc);
   }
 }
 
