@@ -246,9 +246,11 @@ __device__ __forceinline__ void infinite_scores(const SmScores& S, int64_t a0, i
 #pragma unroll
     for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
+      for (int r = 0; r < 16; ++r) {
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb) acc[ib][jb][r] = mine == ib * 32 + (r & 3) + 8 * (r >> 2) ? s[jb] : acc[ib][jb][r];
+        __builtin_amdgcn_sched_barrier(0);                   // (a mask at a time: 64 of them leave no scalar register)
+      }
   }
 #pragma unroll 1
   for (int c = 0; c < 64 * JB; ++c) {
