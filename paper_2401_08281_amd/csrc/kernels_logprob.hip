@@ -1239,6 +1239,14 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
   const int64_t k0 = kblocks * split / splits, k1 = kblocks * (split + 1) / splits;
   const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
   f32x16 acc[4][2] = {};
+  float row_bias[2] = {0.f, 0.f};                     // (asked for before the sums: behind them every store would wait for it)
+  if (DIRECT && bias) {
+#pragma unroll
+    for (int jb = 0; jb < 2; ++jb) {
+      const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
+      row_bias[jb] = bias[b < B.rows ? b : B.rows - 1];
+    }
+  }
   const char* pa = static_cast<const char*>(A.p) + a0 * A.row_bytes;
   const char* pb = static_cast<const char*>(B.p) + b0 * B.row_bytes;
   const int ra_max = (int)(A.rows - 1 - a0 < kBigTile ? A.rows - 1 - a0 : kBigTile - 1);
@@ -1308,7 +1316,7 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
     const int64_t b = b0 + wb * 64 + jb * 32 + (lane & 31);
     if (b >= B.rows) continue;
     if constexpr (DIRECT) {
-      const bool gone = bias && bias[b] == neg_inf();
+      const bool gone = row_bias[jb] == neg_inf();
 #pragma unroll
       for (int ib = 0; ib < 4; ++ib)
 #pragma unroll
@@ -1317,7 +1325,10 @@ __global__ __launch_bounds__(512, 1) void sm_product_kernel(SmMatrix A, SmMatrix
           if (a >= d) continue;
           float v[4];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) v[u] = a + u < d && !gone ? acc[ib][jb][r + u] * sa[a + u] * alpha : 0.f;
+          for (int u = 0; u < 4; ++u) {
+            v[u] = a + u < d ? acc[ib][jb][r + u] * sa[a + u] * alpha : 0.f;
+            v[u] = gone ? 0.f : v[u];
+          }
           store_4(part, b * d + a, d - a, (d & 3) == 0, dtype, v);
         }
       continue;
