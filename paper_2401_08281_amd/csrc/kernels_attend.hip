@@ -22,21 +22,12 @@
 namespace {
 
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kRound = 2048;        // rows of a round
 constexpr int kSegments = 64;       // lists it may span
 constexpr int kTiles = kRound / 64 + kSegments;   // runs of up to 64 rows of one list
 constexpr int kWaves = 4;
 constexpr int kCodeRun = 72;        // bytes of a staged run of 64 rows' codes (18 words: runs start in different banks)
-// (the same in all lanes, and known to be: what follows from it is scalar)
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-__device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
-  return v;
-}
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int w = 32; w > 0; w >>= 1) v = fmaxf(v, __shfl_xor(v, w));
@@ -73,15 +64,6 @@ struct ScanArgs {
 // Rows [first, first + len) of a round; first is a multiple of eight, and weights up to the next one are zero.
 struct Segment { int64_t pos; int32_t list, first, len, pad; };
 struct Tile { int64_t pos; int32_t first, len_seg; };              // a run: length, segment << 8
-
-// The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
-// not wait for them, and the compiler does not always count the wait states across the end of a loop.  A 16x16x32 product's
-// 4 passes are over after 8, any other one's here after fewer than 20.
-__device__ __forceinline__ void settle_products() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
 
 // Groups of lanes that a wavefront's 64 rows are shared out to: 1, 2, 4 or 8 (eight rows each at least)
 __device__ __forceinline__ int row_groups(int mh) { return mh > 32 ? 1 : (mh > 16 ? 2 : (mh > 8 ? 4 : 8)); }
@@ -747,17 +729,10 @@ __host__ __device__ inline TileLds tile_lds(const IvfpqDims& g, int dk, int v0, 
   return o;
 }
 
-// The power of two that brings `mx` into [1, 2), as factor up and its inverse
-__device__ __forceinline__ void unit_scale(float mx, float* up, float* down) {
-  int e = mx > 0.f && mx < __builtin_inff() ? 1 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
-  e = e < -120 ? -120 : (e > 120 ? 120 : e);
-  *up = __builtin_ldexpf(1.f, e);
-  *down = __builtin_ldexpf(1.f, -e);
-}
-// The exponent of the power of two that brings `mx` into [2^14, 2^15)
-__device__ __forceinline__ int top_exponent(float mx) {
-  const int e = mx > 0.f && mx < __builtin_inff() ? 15 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
-  return e < -126 ? -126 : (e > 126 ? 126 : e);
+// A power of two p with p <= mx < 2 p (1 for 0)
+__device__ __forceinline__ float power_below(float mx) {
+  const int e = mx > 0.f && mx < __builtin_inff() ? (int)__builtin_amdgcn_frexp_expf(mx) - 1 : 0;
+  return __builtin_ldexpf(1.f, e < -120 ? -120 : (e > 120 ? 120 : e));
 }
 __device__ __forceinline__ u32 pack_parts(float v) {     // {head, tail}
   const _Float16 hi = (_Float16)v, lo = (_Float16)(v - (float)hi);
@@ -996,9 +971,8 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
     if (q_row) put_query_fragments<W, PL>(ldsb + L.qf, K, NQ, ql, qg, q_row, A.dtype, dsub, kexp, e);
     if (GRAD) {
       const int ge = top_exponent(gx);
-      float bup, bdown;
-      unit_scale(g1 * 32768.f, &bup, &bdown);                // |<g, t>| <= sum |g_t| max |t| < 2 bdown
-      if (qg == 0) { stat[QT + ql] = __builtin_ldexpf(1.f, -ge); stat[2 * QT + ql] = bdown; }
+      // |<g, t>| <= sum |g_t| max |t|, below twice the last one
+      if (qg == 0) { stat[QT + ql] = __builtin_ldexpf(1.f, -ge); stat[2 * QT + ql] = power_below(g1 * 32768.f); }
       if (g_row) put_query_fragments<W, PL>(ldsb + L.gf, V, NQ, ql, qg, g_row, A.dtype, dsub, vexp, ge);
     }
   }

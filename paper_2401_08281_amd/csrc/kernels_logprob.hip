@@ -17,13 +17,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.44269504088896340736f;
-// (the same in all lanes, and known to be: what follows from it is scalar)
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-// e^t for t <= 0 (v_exp_f32: one unit in the last place, results below 2^-126 flush to 0 or a denormal, both fine here)
-__device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
-
 // One score t below the maximum of its group: its weight into l, weight times t into h.  Scores of -inf weigh nothing; a
 // NaN stays one in l.
 __device__ __forceinline__ void softmax_add(float t, float* l, float* h) {
@@ -46,16 +39,6 @@ template <> struct Elem<2> { typedef __bf16 T; };
 
 template <typename T>
 __device__ __forceinline__ float to_f32(T v) { return (float)v; }
-
-// The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
-// not wait for them, and the compiler, which counts the wait states in between, has left them out where it copied an
-// accumulator at the start of the block behind the loop (v_accvgpr_read one instruction after the product: a stale
-// value).  A 32x32x16 product's 8 passes are over after 12 wait states, any other one's here after fewer than 20.
-__device__ __forceinline__ void settle_products() {
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-}
 
 // ---- tiles -------------------------------------------------------------------------
 // A workgroup of four wavefronts takes 256 rows by 128 queries, a wavefront 128 x 64 of them: 12 fragment reads from LDS
@@ -565,12 +548,6 @@ __global__ __launch_bounds__(256) void sm_scores_few_kernel(const typename Elem<
 }
 
 // ---- finish: records -> normaliser, entropy, targets, alternatives ------------------------
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
-  return v;
-}
-
 // <q, x_j> for eight rows at once, eight lanes a row; every lane of a row's group gets the sum.  LANES = 64: one row.
 template <int LANES, typename T>
 __device__ __forceinline__ float dot_rows(const T* __restrict__ q, const T* __restrict__ row, int d) {
@@ -807,12 +784,8 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
 }
 
 // ---- preparation of operands ------------------------------------------------------------
-// The power of two that brings a largest component of `mx` into [2^14, 2^15), the top of fp16's range: what lies 2^28 below
-// it still has its head's full 11 bits, and half a step of the smallest numbers, 2^-25, is 2^-39 of the largest component.
-// A head and a tail together keep 2^-24 of a component, as fp32 does, down to 2^-15 of the largest.
 __device__ __forceinline__ void row_scale(float mx, float* up, float* down) {
-  int e = mx > 0.f && mx < __builtin_inff() ? 15 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
-  e = e < -120 ? -120 : (e > 120 ? 120 : e);
+  const int e = top_exponent(mx);
   *up = __builtin_ldexpf(1.f, e);
   *down = __builtin_ldexpf(1.f, -e);
 }
@@ -1540,9 +1513,8 @@ void launch_sm_gradients(const SmForm& f, bool direct, const SmScores& s, const 
     else if (direct && f.dtype == 2) run(sm_gradients_kernel<1, true, 2, 1>, 2, 1, n);
     else run(sm_gradients_kernel<1, false, 2, 1>, 2, 1, n);
   } else {
-    const int n = tile_lds<4, 2>();
-    if (f.planes == 2) run(sm_gradients_kernel<2, false, 4, 2>, 4, 2, n);
-    else if (direct && f.dtype == 2) run(sm_gradients_kernel<1, true, 4, 2>, 4, 2, n);
+    const int n = tile_lds<4, 2>();                       // (one plane: sm_gradients_small)
+    if (direct && f.dtype == 2) run(sm_gradients_kernel<1, true, 4, 2>, 4, 2, n);
     else run(sm_gradients_kernel<1, false, 4, 2>, 4, 2, n);
   }
 }

@@ -14,6 +14,35 @@ inline dim3 grid_2d(int64_t n) {
 }
 __device__ __forceinline__ int64_t group_id() { return blockIdx.x + (int64_t)gridDim.x * blockIdx.y; }
 
+// ---- what the kernels of both files share ------------------------------------------
+constexpr float kLog2e = 1.44269504088896340736f;
+// (the same in all lanes, and known to be: what follows from it is scalar)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+// e^t for t <= 0 (v_exp_f32: one unit in the last place, results below 2^-126 flush to 0 or a denormal, both fine here)
+__device__ __forceinline__ float exp_neg(float t) { return __builtin_amdgcn_exp2f(t * kLog2e); }
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int w = 32; w > 0; w >>= 1) v += __shfl_xor(v, w);
+  return v;
+}
+// The exponent of the power of two that brings a largest component of `mx` to [2^14, 2^15), the top of fp16's range: what lies
+// 2^28 below it still has its head's full 11 bits, and half a step of the smallest numbers, 2^-25, is 2^-39 of the largest
+// component.  A head and a tail together keep 2^-24 of a component, as fp32 does, down to 2^-15 of the largest.
+__device__ __forceinline__ int top_exponent(float mx) {
+  const int e = mx > 0.f && mx < __builtin_inff() ? 15 - (int)__builtin_amdgcn_frexp_expf(mx) : 0;
+  return e < -126 ? -126 : (e > 126 ? 126 : e);
+}
+// The end of a loop body whose last matrix instructions' results may be read right behind the loop: the hardware does
+// not wait for them, and the compiler, which counts the wait states in between, has left them out where it copied an
+// accumulator at the start of the block behind the loop (v_accvgpr_read one instruction after the product: a stale
+// value).  A 32x32x16 product's 8 passes are over after 12 wait states, any other one's here after fewer than 20.
+__device__ __forceinline__ void settle_products() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // ---- log-probabilities over rows (kernels_logprob.hip) ---------------------------
 // A matrix as the matrix cores read it: rows of whole 128-byte K blocks (two units of 64 bytes), `rows` of them that
 // exist.  A K unit holds 32 fp16 or bf16 elements, or (planes == 2) 16 fp16 heads and behind them their 16 fp16 tails.
