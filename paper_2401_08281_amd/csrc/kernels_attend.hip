@@ -749,6 +749,16 @@ __device__ __forceinline__ void pack_4(const float (&v)[4], u32 (&hi)[2], u32 (&
     lo[i] = __builtin_bit_cast(u32, l);
   }
 }
+// What pack_4 left of the four: heads, and tails too where PL is 2
+template <int PL>
+__device__ __forceinline__ void packed_4(const u32 (&hi)[2], const u32 (&lo)[2], float (&v)[4]) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = (float)__builtin_bit_cast(f16x2, hi[i >> 1])[i & 1];
+    if (PL == 2) v[i] += (float)__builtin_bit_cast(f16x2, lo[i >> 1])[i & 1];
+  }
+}
 __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
@@ -1036,9 +1046,8 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
       float p = 0.f, w = 0.f;
 #pragma unroll
       for (int v = 0; v < 4; ++v) { p += red[(v * 2) * QT + qb * 16 + col]; if (GRAD) w += red[(v * 2 + 1) * QT + qb * 16 + col]; }
-      sum[qb] += p;                              // (sums times 2^14; o also times its component's power, and w over its bound)
-      sum2[qb] += w;
-      const float ws = GRAD ? w * fw[qb] : 0.f;
+      sum[qb] += p;                              // (sums times 2^14; o also times its component's power; lw and o of w over its bound)
+      if (GRAD) sum2[qb] = __builtin_fmaf(w, stat[2 * QT + qb * 16 + col], sum2[qb]);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -1046,7 +1055,7 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
           const int t = (nb * 4 + wave) * 16 + 4 * g + r;
           const float cv = t < nout ? __builtin_ldexpf(c[t], oexp[t]) : 0.f;
           o[SETS - 1][nb][qb][r] = __builtin_fmaf(cv, p, o[SETS - 1][nb][qb][r]);
-          if (GRAD) o[0][nb][qb][r] = __builtin_fmaf(cv, ws, o[0][nb][qb][r]);
+          if (GRAD) o[0][nb][qb][r] = __builtin_fmaf(cv, w, o[0][nb][qb][r]);
         }
     }
     __syncthreads();
@@ -1242,14 +1251,23 @@ __global__ __launch_bounds__(256, SETS_OF(GRAD) * NQ * NB > 12 ? 1 : 2) void att
           if (!((sees >> (qb * 4 + r)) & 1u)) p[r] = 0.f;
           w[r] = p[r] * (t[qb][r] * fg[qb]);
           if (!((sees >> (qb * 4 + r)) & 1u)) w[r] = 0.f;
-          lw[qb] += w[r];
           w[r] *= fw[qb];
+        } else {
+          lp[qb] += p[r];
         }
-        lp[qb] += p[r];
       }
       u32 ph[2], pl[2], wh[2], wl[2];
       pack_4(p, ph, pl);
-      if (GRAD) pack_4(w, wh, wl);
+      if (GRAD) {
+        // Summed as they are multiplied: sum w k and (sum w / sum p) sum p k nearly cancel where few rows have any weight, and
+        // the roundings of the weights must do so with them.
+        pack_4(w, wh, wl);
+        float pk[4], wk[4];
+        packed_4<PL>(ph, pl, pk);
+        packed_4<PL>(wh, wl, wk);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { lp[qb] += pk[r]; lw[qb] += wk[r]; }
+      }
       char* out = ldsb + L.p + (SETS - 1) * L.p_set + (qb * 16 + col) * L.p_stride + row * 2;
       *reinterpret_cast<u32x2*>(out) = u32x2{ph[0], ph[1]};
       if (PL == 2) *reinterpret_cast<u32x2*>(out + QT * L.p_stride) = u32x2{pl[0], pl[1]};
