@@ -98,7 +98,8 @@ VS_API int vs_flat_logprob_grad(const void* x, int64_t nb, const void* q, int64_
  * less than 2^40 of it; the weights are then held in 22 bits, for fp16 and bf16 queries in 11.
  * The index is not written.  With 0 < nprobe < nlist the coarse quantizer uses the index's own work space, as
  * vs_ivfpq_search does: such calls on one index must not overlap in time, the first of a size allocates, and a stream under
- * capture is refused (VS_ERR_UNSUPPORTED).
+ * capture is refused (VS_ERR_UNSUPPORTED).  A captured call holds the addresses of the index's storage: its graph must not be
+ * replayed once vectors have been added to the index, or the index is destroyed.
  * Errors: null pointers (with nq > 0), an index with another metric or with 8-bit codes (VS_ERR_UNSUPPORTED), dk or v0
  * outside their range or inside a sub-quantizer, nprobe outside [0, VS_MAX_K], scale not finite, misaligned vectors or work space, a
  * work space that is too small, an index of another device than the current one; VS_ERR_UNSUPPORTED where the tables of a

@@ -11,8 +11,8 @@
 // column of its wavefront's H only, so additions keep their order and banks never collide.  (Additions by LDS atomics ran
 // at 24 cycles a wavefront, three times the whole scan.)  Partial results of the parts are joined by a second kernel.
 // Bound by LDS: one look-up of QB values, and one of a codeword or a histogram cell, for every code.  1000 queries x 7812
-// codes of 64 sub-quantizers (histograms) 457 us, 2.2 look-ups a ns; gradient of 333 queries x 3200 codes of 32 (codewords)
-// 81 us, 1.3; one query x 4097 codes 20 us, its set-up and two rounds.
+// codes of 64 sub-quantizers (histograms) 460 us, 2.2 look-ups a ns; gradient of 333 queries x 3200 codes of 32 (codewords)
+// 81 us, 1.3; one query x 4097 codes 21 us, its set-up and two rounds.
 #include <algorithm>
 
 #include "../../include/vs_softmax.h"
@@ -672,8 +672,8 @@ __global__ __launch_bounds__(256) void attend_scan_kernel(ScanArgs A) {
 // The gradient's tile computes p from lse and the product of g with the values, w = p <g, t> and adds w k and p k; both
 // relative to the centroid part of <g, v> of the present list, which is exchanged when the list changes.
 // Bound by nothing alone: of a tile's time the score products, the weighted products, the staging of codes and the maxima
-// take a fifth to a third each, and they meet at three barriers.  8 queries x 131,072 codes of 64 sub-quantizers, 128 and 128
-// components: 29 us; 2048 x 16,384 under causal limits 108 us, the gradient of 1024 of them 115 us.
+// take a fifth to a third each, and they meet at two barriers.  8 queries x 131,072 codes of 64 sub-quantizers, 128 and 128
+// components: 31 us; 2048 x 16,384 under causal limits 110 us, the gradient of 1024 of them 118 us.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -1478,7 +1478,10 @@ void tiles_plan(const IvfpqDims& g, int64_t ntotal, int64_t nq, int dk, int v0, 
   p->tiles = true;
   p->fits = true;
   p->qb = 16 * p->nq16;
-  // Parts for three workgroups a CU (2048 queries on 16,384 codes: 256 workgroups 175 us, 512 122, 768 118, 1024 140)
+  // Parts for three workgroups a CU.  Workgroups in all and us of a call: 2048 queries on 16,384 codes under causal limits 256
+  // 175, 512 122, 768 118, 1024 140; one tile of 8 queries on 131,072 codes 256 42.4, 512 38.2, 768 38.1, 1024 38.2; on 524,288
+  // 112, 75, 73 and 92; on 2,000,000 373, 226, 188 and 235; 300 queries (5 tiles) on 65,536 128, 135, 115 and 133.  One tile of
+  // 64 queries, of which two fit a CU, on 524,288: 164, 114, 153 and 144; up to 131,072 codes the least part decides.
   const int64_t groups = (nq + p->qb - 1) / p->qb, want = (768 + groups - 1) / groups;
   const int64_t most = (ntotal + 255) / 256, splits = want < most ? want : most;
   p->per = ((ntotal + splits - 1) / splits + 63) / 64 * 64;

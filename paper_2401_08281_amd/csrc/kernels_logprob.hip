@@ -315,7 +315,7 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
 // ---- forward: scores -> softmax records ---------------------------------------------
 // Bound by the matrix cores for long vectors and by the epilogue's exponentials (some 12 vector instructions per score)
 // for short ones: bf16 4096 x 65,536 x 768 445 to 520 us with the clock, 790 to 930 TFLOP/s (the library's product of these
-// sizes, stored, runs at 976); fp32 1000 x 200,003 x 100 in three products 246 us.  A wavefront's 128 rows are a record of
+// sizes, stored, runs at 976); fp32 1000 x 200,003 x 100 in three products 251 us.  A wavefront's 128 rows are a record of
 // each of its 64 queries.
 template <int PLANES, bool BF16, bool SECOND>
 __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords R, int64_t ta, int64_t tb) {
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords
 // Up to 64 queries the rows are what there is to read: a wavefront loads fragments of 32 rows straight from memory
 // (no LDS, 16 bytes a lane and load) and multiplies them with all queries, whose fragments wait in LDS; four wavefronts
 // make the record of 128 rows.  fp32 rows use v_mfma_f32_16x16x4_f32: exact products, and its 157 TFLOP/s are far above
-// what the stream of rows can ask for.  Bound by memory: bf16 100,003 x 768, one query, 32.8 us, 4.7 TB/s as a copy has.
+// what the stream of rows can ask for.  Bound by memory: bf16 100,003 x 768, one query, 33.3 us, 4.6 TB/s for a copy's 4.7.
 // In the 16x16 layouts a lane holds row lane & 15 of A, and of the result column lane & 15 and rows 4 (lane >> 4) + r.
 template <int DT>
 struct FewMul {
@@ -625,7 +625,7 @@ __device__ __forceinline__ void wave_take_best(const float4 (&rec)[kTakePer], in
 // Where that would be common (few records, or many alternatives) the scores have been kept, and are read instead.
 // TAKE: up to kTakeBest alternatives of up to 256 kTakePer records (262,144 rows), which stay in registers and are picked
 // one by one; more go through the reservoir selection, whose first sort alone takes some 700 instructions.  A chain of
-// latencies: one query of 782 records, k = 10, 11.7 us; 4096 queries of 512 records, k = 5, 61 us.
+// latencies: one query of 782 records, k = 10, 12.1 us; 4096 queries of 512 records, k = 5, 62 us.
 template <int DT, bool TAKE>
 __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R) {
   typedef typename Elem<DT>::T T;
@@ -1031,7 +1031,7 @@ __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, in
 
 // Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
 // G / bound 2^14 in fp16: a value keeps 11 bits (22 with a tail) down to 2^-28 of the bound and 2^-38 of it below.
-// Bound by the matrix cores and the stores of G: bf16 4096 x 16,384 x 768 207 us, 500 TFLOP/s beside 268 MB at 1.3 TB/s.
+// Bound by the matrix cores and the stores of G: bf16 4096 x 16,384 x 768 212 us, 490 TFLOP/s beside 268 MB at 1.3 TB/s.
 template <int PLANES, bool BF16, int IB, int JB>
 __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut O, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
@@ -1193,7 +1193,7 @@ __device__ __forceinline__ void store_4(void* p, int64_t i, int n, bool whole, i
 // out[b][a] = sum_k A[a][k] B[b][k] over long K: tiles of 256 x 256, eight wavefronts of 128 x 64 each.  Against 128 x 128
 // tiles a K block reads three quarters of the LDS per product, and its 2048 cycles of products a SIMD cover the way of the
 // next block from the last-level cache.  Fragments of the next 16 K elements are read while the present ones multiply.
-// 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 141 us: 710 and 730 TFLOP/s.
+// 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 144 us: 710 and 715 TFLOP/s.
 constexpr int kBigTile = 256;
 constexpr int kBigStage = 2 * kBigTile * 128;
 // With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type, zeros

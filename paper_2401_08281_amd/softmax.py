@@ -1,7 +1,9 @@
 """ctypes binding of libvs_softmax.so: same names as the C ABI in include/vs_softmax.h.
 
 Argument marshalling only, as in binding.py.  Work space comes from torch's allocator, on the current
-stream of the tensors' device, so a call can be captured into a graph.
+stream of the tensors' device, so a call can be captured into a graph (of attention: as long as nothing is
+added to the index).  Nothing here is recorded by torch's autograd, whatever its tensors require: results
+are leaves, and a training loop calls the *_grad functions, which return gradients.
 """
 import ctypes
 import os
