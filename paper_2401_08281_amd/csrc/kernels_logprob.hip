@@ -193,68 +193,81 @@ __device__ __forceinline__ Best join_mixed(Best a, Best b) {
   return o;
 }
 
-// <x_a, q_b> of the vectors themselves
-__device__ __forceinline__ float raw_dot(const void* x, int64_t a, const void* q, int64_t b, int d, int dtype) {
+// A component of a vector of any type
+__device__ __forceinline__ float raw_component(const void* p, int64_t i, int dtype) {
+  if (dtype == VS_FP32) return static_cast<const float*>(p)[i];
+  if (dtype == VS_FP16) return (float)static_cast<const _Float16*>(p)[i];
+  return (float)static_cast<const __bf16*>(p)[i];
+}
+// The components of vector a (the same in all lanes) that are infinite or NaN, times those of vector b (a lane's own): what the
+// product of the two comes to, if b is finite elsewhere.
+__device__ __forceinline__ float infinite_dot(const void* pa, int64_t a, const void* pb, int64_t b, int d, int dtype) {
+  const int lane = lane_id();
   float s = 0.f;
-  for (int k = 0; k < d; ++k) {
-    const int64_t i = a * d + k, j = b * d + k;
-    float u, v;
-    if (dtype == VS_FP32) { u = static_cast<const float*>(x)[i]; v = static_cast<const float*>(q)[j]; }
-    else if (dtype == VS_FP16) { u = (float)static_cast<const _Float16*>(x)[i]; v = (float)static_cast<const _Float16*>(q)[j]; }
-    else { u = (float)static_cast<const __bf16*>(x)[i]; v = (float)static_cast<const __bf16*>(q)[j]; }
-    s = __builtin_fmaf(u, v, s);
+  for (int k0 = 0; k0 < d; k0 += 64) {
+    const float v = k0 + lane < d ? raw_component(pa, a * d + k0 + lane, dtype) : 0.f;
+    for (u64 m = __ballot(!(fabsf(v) < __builtin_inff())); m; m &= m - 1) {
+      const int t = __ffsll(m) - 1;
+      s = __builtin_fmaf(__shfl(v, t), raw_component(pb, b * d + k0 + t, dtype), s);
+      if (__ballot(s == s) == 0) return s;                  // (NaN for all)
+    }
   }
   return s;
 }
 
-// The scores of rows and queries with an infinite component, once more from the vectors: a head and a tail cannot hold one
-// (its product with a tail of the other side has any sign), nor can a row be scaled by it.  A row, then a query at a time;
-// no workgroup without such a row or query comes here.
+// The products of rows and queries with an infinite component, once more from the vectors: a head and a tail cannot hold an
+// infinity (its product with a tail of the other side has any sign).  All of them are infinite or NaN, which the infinite
+// factors of these rows and queries leave so.  A row, then a query at a time; a wavefront without either does not come here.
+// row_bits: which of its rows, 64 to a word.
 template <int IB, int JB>
-__device__ __forceinline__ void infinite_scores(const SmScores& S, int64_t a0, int64_t b0, const float2* rowdata, f32x16 (&acc)[IB][JB]) {
-  const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1, half = lane >> 5;
-  float* patch = const_cast<float*>(reinterpret_cast<const float*>(rowdata + 64 * IB)) + 4;       // [64 max(IB, JB)]
+__device__ __forceinline__ void infinite_products(const SmScores& S, int64_t a0, int64_t b0, const float2* rowdata,
+                                                const u64* row_bits, f32x16 (&acc)[IB][JB]) {
+  const int lane = lane_id(), wave = wave_id(), half = lane >> 5;
+  const float2* mine = rowdata + (wave & 1) * 32 * IB;
+  a0 += (wave & 1) * 32 * IB;
+  b0 += (wave >> 1) * 32 * JB;
+  const int64_t lane_q = b0 + lane % (32 * JB) < S.nq ? b0 + lane % (32 * JB) : S.nq - 1;
 #pragma unroll 1
-  for (int i = 0; i < 64 * IB; ++i) {
-    const float2 rd = rowdata[i];                                        // (the same for all)
-    if (rd.x < __builtin_inff() || rd.y == neg_inf()) continue;
-    __syncthreads();
-    if (threadIdx.x < 64 * JB && b0 + threadIdx.x < S.nq)
-      patch[threadIdx.x] = raw_dot(S.raw_x, a0 + i, S.raw_q, b0 + threadIdx.x, S.d, S.dtype) * S.scale + rd.y;
-    __syncthreads();
-    float s[JB];
+  for (int h = 0; h < IB / 2; ++h) {
+    for (u64 m = row_bits[(wave & 1) * (IB / 2) + h]; m; m &= m - 1) {
+      const int i = h * 64 + __ffsll(m) - 1;
+      const float v = infinite_dot(S.raw_x, a0 + i, S.raw_q, lane_q, S.d, S.dtype);
+      float s[JB];
 #pragma unroll
-    for (int jb = 0; jb < JB; ++jb) s[jb] = patch[(wb * JB + jb) * 32 + (lane & 31)];
-    const int mine = i - wa * 32 * IB - 4 * half;
+      for (int jb = 0; jb < JB; ++jb) s[jb] = __shfl(v, jb * 32 + (lane & 31));
+      const int at = i - 4 * half;
 #pragma unroll
-    for (int ib = 0; ib < IB; ++ib)
+      for (int ib = 0; ib < IB; ++ib)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < 16; ++r) {
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb) acc[ib][jb][r] = mine == ib * 32 + (r & 3) + 8 * (r >> 2) ? s[jb] : acc[ib][jb][r];
-        __builtin_amdgcn_sched_barrier(0);                   // (a mask at a time: 64 of them leave no scalar register)
-      }
-  }
-#pragma unroll 1
-  for (int c = 0; c < 64 * JB; ++c) {
-    if (b0 + c >= S.nq || S.q.scale[b0 + c] < __builtin_inff()) continue;
-    __syncthreads();
-    if (threadIdx.x < 64 * IB) {
-      const float b = rowdata[threadIdx.x].y;
-      patch[threadIdx.x] = b == neg_inf() ? neg_inf() : raw_dot(S.raw_x, a0 + threadIdx.x, S.raw_q, b0 + c, S.d, S.dtype) * S.scale + b;
+          for (int jb = 0; jb < JB; ++jb) acc[ib][jb][r] = at == ib * 32 + (r & 3) + 8 * (r >> 2) ? s[jb] : acc[ib][jb][r];
+          __builtin_amdgcn_sched_barrier(0);                 // (a mask at a time: 64 of them leave no scalar register)
+        }
     }
-    __syncthreads();
-#pragma unroll
-    for (int ib = 0; ib < IB; ++ib)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float s = patch[(wa * IB + ib) * 32 + (r & 3) + 8 * (r >> 2) + 4 * half];
-#pragma unroll
-        for (int jb = 0; jb < JB; ++jb)
-          if ((wb * JB + jb) * 32 + (lane & 31) == c) acc[ib][jb][r] = s;
-      }
   }
-  __syncthreads();
+#pragma unroll
+  for (int jb = 0; jb < JB; ++jb) {
+    const int64_t qi = b0 + jb * 32 + (lane & 31);
+    for (u64 m = __ballot(lane < 32 && qi < S.nq && S.q.scale[qi < S.nq ? qi : 0] == __builtin_inff()); m; m &= m - 1) {
+      const int c = __ffsll(m) - 1;
+      float v[IB / 2];
+#pragma unroll
+      for (int h = 0; h < IB / 2; ++h) {
+        const int64_t j = a0 + h * 64 + lane;
+        v[h] = infinite_dot(S.raw_q, b0 + jb * 32 + c, S.raw_x, j < S.nx ? j : S.nx - 1, S.d, S.dtype);
+      }
+#pragma unroll
+      for (int ib = 0; ib < IB; ++ib)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = ib * 32 + (r & 3) + 8 * (r >> 2) + 4 * half;
+          const float s = __shfl(v[ib / 2], i & 63) + (mine[i].x == __builtin_inff() ? acc[ib][jb][r] : 0.f);   // (both: both count)
+          if ((lane & 31) == c) acc[ib][jb][r] = s;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
 }
 
 // The scores of a wavefront's tile in place of its products: s = acc * (row factor * query factor) + bias, -inf for
@@ -264,15 +277,17 @@ template <int IB, int JB>
 __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int64_t b0, float2* rowdata, f32x16 (&acc)[IB][JB]) {
   const int lane = lane_id(), wave = wave_id(), wa = wave & 1, wb = wave >> 1;
   const bool plain = S.x.scale == nullptr && S.bias == nullptr && a0 + 64 * IB <= S.nx;   // (the same in the workgroup)
+  u64* row_bits = reinterpret_cast<u64*>(rowdata + 64 * IB);             // [IB] rows with an infinity that take part
   float cq[JB];
-  bool odd = false;                                                      // an infinite component takes part
+  bool odd = false;                                                      // (queries likewise)
 #pragma unroll
   for (int jb = 0; jb < JB; ++jb) {
     const int64_t qi = b0 + (wb * JB + jb) * 32 + (lane & 31);
     cq[jb] = S.q.scale && qi < S.nq ? S.q.scale[qi] * 0x1p14f : 1.f;
-    odd = odd || !(cq[jb] < __builtin_inff());
+    odd = odd || cq[jb] == __builtin_inff();
     cq[jb] *= S.scale;
   }
+  u64 any = __ballot(odd);
   if (!plain) {
     const int64_t j = a0 + threadIdx.x;
     if (threadIdx.x < 64 * IB) {
@@ -282,13 +297,14 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
         b = S.bias ? S.bias[j] : 0.f;
       }
       rowdata[threadIdx.x] = make_float2(xs, b);
-      odd = odd || (b != neg_inf() && !(xs < __builtin_inff()));
-    }
-    if (S.raw_x) {                                             // (a word of every wavefront)
-      const u64 any = __ballot(odd);
-      if (lane == 0) reinterpret_cast<u32*>(rowdata + 64 * IB)[wave] = any != 0 ? 1u : 0u;
+      const u64 bits = __ballot(b != neg_inf() && xs == __builtin_inff());
+      if (lane == 0) row_bits[wave] = bits;
     }
     __syncthreads();
+#pragma unroll
+    for (int h = 0; h < IB / 2; ++h) any |= row_bits[wa * (IB / 2) + h];
+    // (ahead of the scores, which are computed and used in one block of instructions)
+    if (__builtin_expect(S.raw_x && __ballot(any != 0) != 0, 0)) infinite_products(S, a0, b0, rowdata, row_bits, acc);
   }
 #pragma unroll
   for (int ib = 0; ib < IB; ++ib)
@@ -306,10 +322,6 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
         }
       }
     }
-  if (!plain && S.raw_x) {
-    const u32x4 any = *reinterpret_cast<const u32x4*>(rowdata + 64 * IB);
-    if (__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]) != 0) infinite_scores(S, a0, b0, rowdata, acc);
-  }
 }
 
 // ---- forward: scores -> softmax records ---------------------------------------------
@@ -753,20 +765,28 @@ __global__ __launch_bounds__(256) void sm_finish_kernel(SmFinish F, SmRecords R)
       if (wave == 0 && lane < F.k) chosen[lane] = key == KEY_EMPTY ? KEY_EMPTY : make_key(key_value(key, 1), lone_row, 1);
       done = true;
     } else {
-      // (the maxima that stand alone are multiplied again as well: equal rows must meet with equal bits)
+      // the maxima that stand alone, then whole records, 32 rows a step (all of them: equal rows must meet with equal bits)
       start();
-      auto again = [&](int64_t j, bool in) {
+      const u64 lone = __ballot(key != KEY_EMPTY && !whole);
+      const int lones = (F.k + 31) / 32, steps = lones + 4 * __popcll(todo);
+      u64 rest = todo;
+      u32 pw = 0;
+      for (int t = 0; t < steps; ++t) {
+        const int i = wave * 8 + group;                     // of the step's rows
+        int64_t j;
+        bool in = true;
+        if (t < lones) {
+          j = __shfl(lone_row, t * 32 + i);
+          in = (lone >> (t * 32 + i)) & 1u;
+        } else {
+          const int r = (t - lones) & 3;
+          if (r == 0) { pw = __shfl(p, __ffsll(rest) - 1); rest &= rest - 1; }
+          j = (int64_t)pw * kSmRecRows + r * 32 + i;
+        }
         in = in && j < F.nb;
         const float b = in ? (F.bias ? F.bias[j] : 0.f) : neg_inf();
         const float s = rank_value(dot_rows<8>(q, x + (in ? j : 0) * F.d, F.d) * F.scale + b);
         sel.push_value((lane & 7) == 0 && b > neg_inf() && s > neg_inf(), s, (u32)j);
-      };
-      const u64 lone = __ballot(key != KEY_EMPTY && !whole);
-      for (int i0 = wave * 8; i0 < F.k; i0 += 32)
-        again(__shfl(lone_row, i0 + group), (lone >> (i0 + group)) & 1u);
-      for (u64 rest = todo; rest; rest &= rest - 1) {
-        const u32 pw = __shfl(p, __ffsll(rest) - 1);
-        for (int r0 = wave * 8; r0 < kSmRecRows; r0 += 32) again((int64_t)pw * kSmRecRows + r0 + group, true);
       }
     }
   }
@@ -823,7 +843,11 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide 
   const bool gone = bias && bias[r] == neg_inf(), kept = dp <= 16 * V * kPrepSteps;
   const T* row = x + r * d;
   float v[kPrepSteps][V];
-  float mx = 0.f;
+  u32 mx = 0;                                                          // the largest size, as bits: a NaN is above infinity
+  auto take = [&](float e) {
+    const u32 b = __float_as_uint(e) & 0x7FFFFFFFu;
+    mx = b > mx ? b : mx;
+  };
   if (kept) {
 #pragma unroll
     for (int i = 0; i < kPrepSteps; ++i) {
@@ -835,18 +859,18 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide 
 #pragma unroll
     for (int i = 0; i < kPrepSteps; ++i)
 #pragma unroll
-      for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[i][u]));
+      for (int u = 0; u < V; ++u) take(v[i][u]);
   } else if (!gone) {
     for (int k = l * V; k < d; k += 16 * V) {
       load_piece(row, k, d, v[0]);
 #pragma unroll
-      for (int u = 0; u < V; ++u) mx = fmaxf(mx, fabsf(v[0][u]));
+      for (int u = 0; u < V; ++u) take(v[0][u]);
     }
   }
 #pragma unroll
-  for (int w = 1; w < 16; w <<= 1) mx = fmaxf(mx, __shfl_xor(mx, w));
+  for (int w = 1; w < 16; w <<= 1) take(__uint_as_float(__shfl_xor(mx, w)));
   float up, down;
-  row_scale(mx, &up, &down);
+  row_scale(__uint_as_float(mx), &up, &down);
   char* out = planes + r * (dp * 2 * PLANES);
   auto put = [&](int64_t k, const float (&e)[V]) {
     _Float16 hi[V], lo[V];
@@ -874,7 +898,8 @@ __global__ __launch_bounds__(256) void sm_prep_rows_kernel(SmSide side0, SmSide 
       put(k, v[0]);
     }
   }
-  if (l == 0) scale[r] = mx < __builtin_inff() ? down : mx;             // (see infinite_scores)
+  // (a NaN makes the row's scores NaN, an infinity leaves them to infinite_products)
+  if (l == 0) scale[r] = mx < 0x7F800000u ? down : __uint_as_float(mx);
 }
 
 // Largest size in every column: a thread goes down 16 bytes of columns, four rows in flight, as many rows beside each

@@ -71,7 +71,7 @@ struct SmSide {
   const float* bias = nullptr;      // rows whose bias is -inf become zeros
   const float* factor = nullptr;    // of every row, for its columns; a row of factor 0 is not read
   void* rows = nullptr;             // out: every row as K blocks of fp16 parts times 1 / row_scale, its largest component in
-  float* row_scale = nullptr;       // [2^14, 2^15); infinite for a row with an infinite component
+  float* row_scale = nullptr;       // [2^14, 2^15); infinite or NaN as its largest component is
   void* cols = nullptr;             // out: every column of (factor x) as K blocks over the rows, likewise
   float* col_scale = nullptr;
   u32* colmax = nullptr;            // [d] of scratch, zeros on entry

@@ -63,3 +63,55 @@ def test_a_query_with_an_infinite_component(vs, nq, dtype, d):
     assert lse[2] == -INF and ent[2] == 0 and (tv[2] == -INF).all() and (ti[2] == -1).all()
     others = torch.arange(nq, device="cuda") != 2
     assert torch.equal(lse[others], clean[1][others]) and torch.equal(ti[others], clean[4][others])
+
+
+@pytest.mark.parametrize("dtype,d", [("fp32", 100), ("fp32", 64), ("bf16", 100), ("fp16", 33), ("fp32", 300)])
+@pytest.mark.parametrize("nq", [40, 65, 300])
+def test_infinities_meet(vs, nq, dtype, d):
+    """One row a call, so that lse is its score: infinities of one sign stay, of both signs are NaN, as is one times zero; in the
+    row, in the query, in both; NaN beside them."""
+    g = torch.Generator().manual_seed(nq + d)
+    q = (torch.randn(nq, d, generator=g) * 4).round() / 4
+    places = torch.randint(0, d, (6,), generator=g)
+    q[::5, places[0]] = INF
+    q[1::7, places[1]] = -INF
+    q[2::11, places[2]] = float("nan")
+    for count in (0, 1, 2, 3):
+        x = (torch.randn(1, d, generator=g) * 4).round() / 4
+        for n in range(count):
+            x[0, places[n + 1]] = INF if n % 2 == 0 else -INF
+        X, Q = x.to(DTYPES[dtype]), q.to(DTYPES[dtype])
+        s = (Q.double() * X.double()).sum(1) * -0.5 + 0.25
+        bias = torch.full((1,), 0.25, device="cuda")
+        lse = vs.vs_flat_logprob(X.cuda(), Q.cuda(), None, 0, -0.5, bias)[1].double().cpu()
+        fin = s.isfinite()
+        assert (lse[fin] - s[fin]).abs().max() < 1e-3 if fin.any() else True
+        assert (lse[s == -INF] == -INF).all() and lse[s.isnan() | (s == INF)].isnan().all()
+
+
+def test_a_table_of_infinities(vs):
+    """Every row holds one, as after a diverged step: the call ends, with what is left for every query."""
+    nb, nq, d = 50_000, 500, 96
+    x, q, _, _ = make(nb, nq, d, torch.float32, 0, False, 9, grid=False)
+    x[:, 11] = torch.where(torch.arange(nb, device="cuda") % 2 == 0, INF, -INF)
+    q[:, 11] = q[:, 11].abs() + 0.25
+    lse = vs.vs_flat_logprob(x, q)[1]
+    assert lse.isnan().all()
+    x[:, 11] = -INF
+    x[nb // 2, 11] = 0.5
+    lse, ent, _, ti = vs.vs_flat_logprob(x, q, None, 3)[1:]
+    want = (q.double() * x[nb // 2].double()).sum(1)
+    assert (lse.double() - want).abs().max() < 1e-3 and (ent == 0).all()
+    assert (ti[:, 0] == nb // 2).all() and (ti[:, 1:] == -1).all()
+
+
+def test_a_table_of_nan(vs):
+    nb, nq, d = 50_000, 500, 96
+    x, q, _, _ = make(nb, nq, d, torch.float32, 0, False, 9, grid=False)
+    x[1:] = float("nan")
+    lse = vs.vs_flat_logprob(x, q)[1]
+    assert lse.isnan().all()
+    bias = torch.full((nb,), -INF, device="cuda")
+    bias[0] = 0.0
+    lse = vs.vs_flat_logprob(x, q, bias=bias)[1]
+    assert (lse.double() - (q.double() * x[0].double()).sum(1)).abs().max() < 1e-3
