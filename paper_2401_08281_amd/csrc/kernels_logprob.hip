@@ -327,7 +327,7 @@ __device__ __forceinline__ void finish_scores(const SmScores& S, int64_t a0, int
 // ---- forward: scores -> softmax records ---------------------------------------------
 // Bound by the matrix cores for long vectors and by the epilogue's exponentials (some 12 vector instructions per score)
 // for short ones: bf16 4096 x 65,536 x 768 445 to 520 us with the clock, 790 to 930 TFLOP/s (the library's product of these
-// sizes, stored, runs at 976); fp32 1000 x 200,003 x 100 in three products 251 us.  A wavefront's 128 rows are a record of
+// sizes, stored, runs at 976); fp32 1000 x 200,003 x 100 in three products 242 to 251 us.  A wavefront's 128 rows are a record of
 // each of its 64 queries.
 template <int PLANES, bool BF16, bool SECOND>
 __global__ __launch_bounds__(256, 2) void sm_scores_kernel(SmScores S, SmRecords R, int64_t ta, int64_t tb) {
@@ -1056,7 +1056,7 @@ __global__ __launch_bounds__(256) void sm_coefs_kernel(SmGrads g, int64_t nq, in
 
 // Scores again, then G in place of them, as operands of the two products that follow: G [nq][rows] and its transpose.
 // G / bound 2^14 in fp16: a value keeps 11 bits (22 with a tail) down to 2^-28 of the bound and 2^-38 of it below.
-// Bound by the matrix cores and the stores of G: bf16 4096 x 16,384 x 768 212 us, 490 TFLOP/s beside 268 MB at 1.3 TB/s.
+// Bound by the matrix cores and the stores of G: bf16 4096 x 16,384 x 768 210 us, 490 TFLOP/s beside 268 MB at 1.3 TB/s.
 template <int PLANES, bool BF16, int IB, int JB>
 __global__ __launch_bounds__(256, 2) void sm_gradients_kernel(SmScores S, SmGOut O, int64_t ta, int64_t tb) {
   extern __shared__ __align__(16) char lds[];
@@ -1218,7 +1218,7 @@ __device__ __forceinline__ void store_4(void* p, int64_t i, int n, bool whole, i
 // out[b][a] = sum_k A[a][k] B[b][k] over long K: tiles of 256 x 256, eight wavefronts of 128 x 64 each.  Against 128 x 128
 // tiles a K block reads three quarters of the LDS per product, and its 2048 cycles of products a SIMD cover the way of the
 // next block from the last-level cache.  Fragments of the next 16 K elements are read while the present ones multiply.
-// 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 144 us: 710 and 715 TFLOP/s.
+// 768 x 4096 over K = 16,384 in 5 splits 145 us, 768 x 16,384 over K = 4096 142 us: 710 and 725 TFLOP/s.
 constexpr int kBigTile = 256;
 constexpr int kBigStage = 2 * kBigTile * 128;
 // With one split and nothing to add to, results go out at once: out[b][a] = alpha sa[a] sum in the vectors' type, zeros
